@@ -18,7 +18,7 @@
  *     dependents start early (programmatic dependent launch: griddepcontrol.launch_dependents,
  *     cudaTriggerProgrammaticLaunchCompletion).  A kernel of the caller's that does so must not write expert tables or
  *     weights, unless other work is enqueued between it and the call: a kernel that does not, a copy, or slicemoe_pack
- *     (not slicemoe_route_topk or another layer call).  Ordinary kernels, copies and slicemoe_pack may write them
+ *     (not slicemoe_route_topk, another layer call, or one of the calls for microscaled experts but slicemoe_mx4_pack).  Ordinary kernels, copies and slicemoe_pack may write them
  *     directly ahead of the call.
  *   - Weight matrices are row-major [N, K] (N outputs, K inputs = contraction axis); quantisation
  *     groups run along K.
@@ -382,6 +382,130 @@ int slicemoe_prefill_layer(const slicemoe_shape *shape, const slicemoe_expert *e
                            int T, const int32_t *ids, const float *weights, const uint8_t *expert_prec,
                            float *y, void *workspace, size_t workspace_bytes, int *status_out_device,
                            void *stream);
+
+/*
+ * Experts in microscaled 4-bit floats, and the routing that goes with them.  (Not part of the paper's method: the paper's
+ * weights are integer codes.  The format is MXFP4 of the OCP Microscaling Formats specification, version 1.0, which the
+ * tensor cores multiply directly, activations and weights alike.)  A layer is: slicemoe_route_scored, slicemoe_mx4_quantize of
+ * the activations, slicemoe_mx4_product with the gated matrices, slicemoe_mx4_quantize of its result, slicemoe_mx4_product with
+ * the down matrices, slicemoe_combine.  The library's binding has that sequence as mx4_expert_ffn.
+ *
+ * Element types of the floating-point arrays of these calls:
+ */
+#define SLICEMOE_F32 0
+#define SLICEMOE_BF16 1
+#define SLICEMOE_F16 2
+
+/*
+ * slicemoe_route_scored - routing to experts by softmax or sigmoid scores, with groups of experts and a bias for balance.
+ *   logits     device [T, E] of `dtype`, rows ld elements apart (ld >= E); a NaN counts as -inf
+ *   score      SLICEMOE_SCORE_SOFTMAX: s = softmax(logits); SLICEMOE_SCORE_SIGMOID: s = 1 / (1 + exp(-logit)).  Where every
+ *              logit of a row is -inf its scores are 0; logits of +inf share a softmax among themselves
+ *   bias       device float32 [E] or NULL: added to the score for SELECTION only (key = s + bias, NaN = -inf)
+ *   n_group, topk_group, group_best   the experts are n_group groups of E / n_group consecutive ones; a group's value is the
+ *              sum of its group_best (1 or 2) largest keys; only experts of the topk_group groups of largest value are
+ *              selected.  n_group = 1: no groups
+ *   k          experts per token, by descending key.  Ties, of groups too, go to the lower index
+ *   renorm     1: the k scores are divided by their sum (weights are 0 where the sum is)
+ *   scale      a factor of the weights, applied last
+ *   tau, rank_high, prec_req   as in slicemoe_route_topk, on the score before renorm and scale
+ *   ids        device int32 [T, k]; weights device float32 [T, k]; prec_req device uint8 [T, k] or NULL
+ * Selection is that of exact arithmetic down to the rounding of 64-bit floats: where keys in 32 bits are too close to tell,
+ * the token's keys are worked out again in 64.  Without a bias experts are ordered by their logits.
+ * Errors: INVALID_ARG (null, T <= 0, k < 1, k > SLICEMOE_MAX_TOP_K, ld < E, E % n_group, topk_group not in [1, n_group],
+ * group_best above a group's size, k > topk_group * E / n_group, logits off their type's alignment), UNSUPPORTED (E > 512,
+ * n_group > 32, group_best not 1 or 2, an unknown dtype or score).
+ */
+#define SLICEMOE_SCORE_SOFTMAX 0
+#define SLICEMOE_SCORE_SIGMOID 1
+int slicemoe_route_scored(const void *logits, int dtype, int T, int E, int64_t ld, int score, const float *bias, int n_group,
+                          int topk_group, int group_best, int k, int renorm, float scale, float tau, int rank_high,
+                          int32_t *ids, float *weights, uint8_t *prec_req, void *stream);
+
+/*
+ * Microscaled 4-bit floats.  32 consecutive values of a row share a scale 2^(b - 127), b a byte (E8M0; b = 255: NaN).  A value is
+ * a sign, two bits of exponent (bias 1) and one of mantissa (E2M1): 0, 0.5, 1, 1.5, 2, 3, 4 or 6 times the scale.
+ *   codes   uint8 [rows, K / 2]: value 2 i in the low four bits of byte i, value 2 i + 1 in the high four
+ *   scale   uint8 [rows, slicemoe_mx4_scale_pitch(K)], K / 32 bytes and then zeros up to a multiple of four
+ *
+ * slicemoe_mx4_quantize - x device [rows, K] of `dtype`, rows ld elements apart.  Per block of 32: 2^e is the power of two at or
+ * below the largest magnitude, the scale is 2^(e - 2) (not below 2^-127), values divided by it are rounded to the nearest of
+ * the above, ties to the even mantissa, magnitudes beyond 6 to 6.  A block that holds an infinity or a NaN gets scale byte 255,
+ * codes 0: all of it reads as NaN.  Exact and deterministic.
+ * slicemoe_mx4_dequantize - the values again, into out [rows, K] of `dtype`, rows ld elements apart (bf16 and fp32 hold every value
+ * exactly; fp16 rounds, and overflows beyond 65504).
+ *   K % 32 == 0; codes 16-byte, scale 4-byte aligned; x and out aligned to their element type.
+ * Errors: INVALID_ARG (null, rows <= 0, K <= 0, K % 32, ld < K, alignment), UNSUPPORTED (dtype), CUDA.
+ */
+size_t slicemoe_mx4_scale_pitch(int K);
+int slicemoe_mx4_quantize(const void *x, int dtype, int rows, int K, int64_t ld, uint8_t *codes, uint8_t *scale, void *stream);
+int slicemoe_mx4_dequantize(const uint8_t *codes, const uint8_t *scale, int rows, int K, void *out, int dtype, int64_t ld,
+                            void *stream);
+
+/*
+ * One matrix of weights [N, K] in that format - or, with `gated`, a pair of them, gate and up - in the layout that
+ * slicemoe_mx4_product reads; the pointers are device pointers, 16-byte aligned.
+ *   Physical layout: rows in blocks of 128 (of a gated pair: 16 rows of gate, the same 16 of up, and so on), K in chunks of 64;
+ *   codes [block][chunk][half of the chunk, 32 values][row of the block][16 bytes], scale [block][ceil(K / 128)][row % 32]
+ *   [row / 32][4 bytes].  Rows and values beyond the matrix are zeros.
+ * slicemoe_mx4_pack - offline preparation: W (and up, of a gated pair; else NULL) device [N, K] of `dtype`, rows ld elements apart,
+ * quantised as by slicemoe_mx4_quantize into buffers of slicemoe_mx4_codes_bytes / slicemoe_mx4_scale_bytes bytes.
+ * slicemoe_mx4_unpack - test hook and dump helper: the codes and scales of gate (part 0; a plain matrix) or up (part 1) as
+ * slicemoe_mx4_quantize writes them.
+ * Errors: INVALID_ARG (null, N <= 0, K <= 0, K % 32, ld < K, alignment), UNSUPPORTED (dtype; N > 2^24 or K > 2^20), CUDA.
+ */
+typedef struct slicemoe_mx4_mat {
+  const uint8_t *codes, *scale;
+  int32_t N, K;
+  int32_t gated, reserved;
+} slicemoe_mx4_mat;
+size_t slicemoe_mx4_codes_bytes(int N, int K, int gated);
+size_t slicemoe_mx4_scale_bytes(int N, int K, int gated);
+int slicemoe_mx4_pack(const void *W, const void *up, int dtype, int N, int K, int64_t ld, uint8_t *codes, uint8_t *scale,
+                      void *stream);
+int slicemoe_mx4_unpack(const uint8_t *codes, const uint8_t *scale, int N, int K, int gated, int part, uint8_t *codes_rm,
+                        uint8_t *scale_rm, void *stream);
+
+/*
+ * slicemoe_mx4_product - rows of activations times the matrices of the experts that a routing list names:
+ *   out[t, j] = W_e x[t]                            e = ids[t, j]
+ *   out[t, j] = silu(gate_e x[t]) * (up_e x[t])     with gated matrices; silu(v) = v / (1 + exp(-v))
+ * on the tensor cores (tcgen05, 4-bit floats with a scale per 32, fp32 accumulation), one token or a long prompt: an expert's
+ * rows are brought together on the device and its matrix is read once for up to 224 of them.
+ *   mats       device array [n_experts]; all of them N x K and gated alike (K % 32 == 0)
+ *   codes, scale   the activations as slicemoe_mx4_quantize writes them: x_per_pair 0: [T, K / 2], a row per token;
+ *              x_per_pair 1: [T k, K / 2], a row per pair (the result of a product before).  The scale bytes behind K / 32 are
+ *              not looked at
+ *   ids        device int32 [T, k]; or NULL: every row is multiplied by mats[0] (k = 1: a product of two matrices)
+ *   out        device [T, k, N] of `dtype`, rounded once from fp32; aligned to 16 bytes.  The row of a pair whose id is outside
+ *              [0, n_experts) is left as it was, and SLICEMOE_STATUS_BAD_EXPERT_ID is set; so it is where the expert's table entry is
+ *              not an N x K matrix of this kind (null pointers, other sizes)
+ *   workspace  device, slicemoe_mx4_workspace_bytes(T, k, n_experts) bytes, 256-byte aligned, prepared once by
+ *              slicemoe_mx4_workspace_init.  slicemoe_get_status reads (and clears) its status word and
+ *              slicemoe_workspace_set_wait sets its wait limit, as for slicemoe_workspace_init's.  It serves one stream at a
+ *              time; two calls that may overlap, or two graphs that may run at once, need one each
+ * A row's result does not depend on the other rows of the call, bit for bit, and is reproducible.
+ * Errors: INVALID_ARG (null, sizes, alignment, workspace too small), UNSUPPORTED (n_experts > 1024, T k > 2^24, N > 2^24,
+ * K > 2^20, k > SLICEMOE_MAX_TOP_K, dtype), CUDA.
+ */
+size_t slicemoe_mx4_workspace_bytes(int T, int k, int n_experts);
+int slicemoe_mx4_workspace_init(void *workspace, size_t workspace_bytes, void *stream);
+int slicemoe_mx4_product(const slicemoe_mx4_mat *mats, int n_experts, int N, int K, int gated, const uint8_t *codes,
+                         const uint8_t *scale, int T, int k, int x_per_pair, const int32_t *ids, void *out, int dtype,
+                         void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * slicemoe_combine - the end of a layer: out[t] = base[t] + sum_j weights[t, j] rows[t, j], added up in fp32 in list order, rounded
+ * once.
+ *   rows       device [T, k, N] of rows_dtype; weights device float32 [T, k]
+ *   ids        device int32 [T, k] or NULL: pairs whose id is outside [0, n_experts) are left out (their rows are not read)
+ *   base       device [T, N] of out_dtype or NULL (a residual, or the shared experts' part); may be out itself
+ *   out        device [T, N] of out_dtype
+ * Arrays are aligned to their element type.  Errors: INVALID_ARG (null, T <= 0, N <= 0, k < 1, n_experts <= 0 with ids,
+ * alignment), UNSUPPORTED (k > SLICEMOE_MAX_TOP_K, an unknown dtype), CUDA.
+ */
+int slicemoe_combine(const void *rows, int rows_dtype, int T, int k, int N, const float *weights, const int32_t *ids,
+                     int n_experts, const void *base, void *out, int out_dtype, void *stream);
 
 /*
  * Host-side Dynamic Bit-Sliced Caching bookkeeping (Section 4.1; cache set-up of Section

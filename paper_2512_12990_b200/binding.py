@@ -37,6 +37,9 @@ EXPORTS = (
     "slicemoe_cost_paper_hw", "slicemoe_cost_step", "slicemoe_dbsc_log_evictions", "slicemoe_dbsc_drain_evicted",
     "slicemoe_tier_sizes", "slicemoe_tier_store_expert", "slicemoe_tier_create", "slicemoe_tier_destroy",
     "slicemoe_tier_cache", "slicemoe_tier_request", "slicemoe_tier_sync", "slicemoe_tier_stats",
+    "slicemoe_route_scored", "slicemoe_mx4_scale_pitch", "slicemoe_mx4_quantize", "slicemoe_mx4_dequantize", "slicemoe_mx4_codes_bytes",
+    "slicemoe_mx4_scale_bytes", "slicemoe_mx4_pack", "slicemoe_mx4_unpack", "slicemoe_mx4_workspace_bytes", "slicemoe_mx4_workspace_init",
+    "slicemoe_mx4_product", "slicemoe_combine",
 )
 
 
@@ -67,6 +70,11 @@ class Mat(Structure):
 
 class Expert(Structure):
     _fields_ = [("gate", Mat), ("up", Mat), ("down", Mat)]
+
+
+class Mx4MatDesc(Structure):
+    _fields_ = [("codes", c_void_p), ("scale", c_void_p), ("N", c_int32), ("K", c_int32), ("gated", c_int32),
+                ("reserved", c_int32)]
 
 
 def lib() -> ctypes.CDLL:
@@ -152,6 +160,22 @@ def lib() -> ctypes.CDLL:
     L.slicemoe_cost_paper_hw.argtypes = [POINTER(CostHw)]
     L.slicemoe_cost_paper_hw.restype = None
     L.slicemoe_cost_step.argtypes = [POINTER(CostHw), c_int64, c_int64, c_int64, POINTER(c_double), POINTER(c_double)]
+    L.slicemoe_route_scored.argtypes = [c_void_p, c_int, c_int, c_int, c_int64, c_int, c_void_p, c_int, c_int, c_int, c_int, c_int,
+                                        c_float, c_float, c_int, c_void_p, c_void_p, c_void_p, c_void_p]
+    for name in ("slicemoe_mx4_scale_pitch", "slicemoe_mx4_codes_bytes", "slicemoe_mx4_scale_bytes", "slicemoe_mx4_workspace_bytes"):
+        getattr(L, name).restype = c_size_t
+    L.slicemoe_mx4_scale_pitch.argtypes = [c_int]
+    L.slicemoe_mx4_codes_bytes.argtypes = [c_int, c_int, c_int]
+    L.slicemoe_mx4_scale_bytes.argtypes = [c_int, c_int, c_int]
+    L.slicemoe_mx4_workspace_bytes.argtypes = [c_int, c_int, c_int]
+    L.slicemoe_mx4_quantize.argtypes = [c_void_p, c_int, c_int, c_int, c_int64, c_void_p, c_void_p, c_void_p]
+    L.slicemoe_mx4_dequantize.argtypes = [c_void_p, c_void_p, c_int, c_int, c_void_p, c_int, c_int64, c_void_p]
+    L.slicemoe_mx4_pack.argtypes = [c_void_p, c_void_p, c_int, c_int, c_int, c_int64, c_void_p, c_void_p, c_void_p]
+    L.slicemoe_mx4_unpack.argtypes = [c_void_p, c_void_p, c_int, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p]
+    L.slicemoe_mx4_workspace_init.argtypes = [c_void_p, c_size_t, c_void_p]
+    L.slicemoe_mx4_product.argtypes = [c_void_p, c_int, c_int, c_int, c_int, c_void_p, c_void_p, c_int, c_int, c_int, c_void_p, c_void_p,
+                                       c_int, c_void_p, c_size_t, c_void_p]
+    L.slicemoe_combine.argtypes = [c_void_p, c_int, c_int, c_int, c_int, c_void_p, c_void_p, c_int, c_void_p, c_void_p, c_int, c_void_p]
     _lib = L
     return L
 
@@ -355,6 +379,137 @@ def slicemoe_prefill_layer(shape: Shape, experts_tbl, shared_tbl, shared_gate_ve
     status a CUDA int32 [1] tensor (read it after synchronising)."""
     return (_m or _marshal()).prefill_layer(shape, experts_tbl, shared_tbl, shared_gate_vec, x, ids, weights, expert_prec, ws,
                                             y, status, stream)
+
+
+# ---- experts in microscaled 4-bit floats, and the routing that goes with them ------------------------------
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
+_SCORES = {"softmax": SCORE_SOFTMAX, "sigmoid": SCORE_SIGMOID}
+F32, BF16, F16 = 0, 1, 2
+
+
+def _dtype_code(t) -> int:
+    import torch
+    codes = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+    if t not in codes:
+        raise ValueError(f"float32, bfloat16 or float16 is wanted, got {t}")
+    return codes[t]
+
+
+def slicemoe_route_scored(logits, k: int, score: str = "softmax", bias=None, n_group: int = 1, topk_group: int = 1, group_best: int = 1,
+                          renorm: bool = False, scale: float = 1.0, tau: float = 2.0, rank_high: int = 0, want_prec: bool = True,
+                          stream=None):
+    """logits CUDA float32, bfloat16 or float16 [T, E], rows may be spaced; score "softmax" or "sigmoid"; bias CUDA float32 [E] or
+    None.  Returns (ids int32 [T, k], weights float32 [T, k], prec_req uint8 [T, k] | None)."""
+    return (_m or _marshal()).route_scored(logits, k, _SCORES[score], bias, n_group, topk_group, group_best, renorm, scale, tau, rank_high,
+                                           want_prec, stream)
+
+
+def slicemoe_mx4_quantize(x, stream=None):
+    """x: CUDA float32, bfloat16 or float16 [..., K], rows may be spaced.  Returns (codes uint8 [..., K / 2], scale uint8 [..., pitch])."""
+    return (_m or _marshal()).mx4_quantize(x, stream)
+
+
+def slicemoe_mx4_dequantize(codes, scale, dtype=None, out=None, stream=None):
+    """codes, scale as slicemoe_mx4_quantize returns them -> values [..., K] of `dtype` (or of `out`, if given)."""
+    return (_m or _marshal()).mx4_dequantize(codes, scale, dtype, out, stream)
+
+
+class Mx4Mat:
+    """Device buffers of one packed matrix, or gated pair of matrices, of microscaled 4-bit floats."""
+
+    def __init__(self, N, K, gated, codes, scale):
+        self.N, self.K, self.gated, self.codes, self.scale = N, K, bool(gated), codes, scale
+
+    def desc(self) -> Mx4MatDesc:
+        return Mx4MatDesc(self.codes.data_ptr(), self.scale.data_ptr(), self.N, self.K, 1 if self.gated else 0, 0)
+
+
+def slicemoe_mx4_pack(W, up=None, stream=None) -> Mx4Mat:
+    """W: CUDA float32, bfloat16 or float16 [N, K] with dense rows; up: the same, for a gated pair (W is then gate)."""
+    import torch
+    for t in (W,) if up is None else (W, up):
+        if not (t.is_cuda and t.dim() == 2 and t.stride(1) == 1 and t.stride(0) >= t.shape[1]) or \
+                (t.shape, t.stride(0), t.dtype, t.device) != (W.shape, W.stride(0), W.dtype, W.device):
+            raise ValueError("CUDA matrices with dense rows, alike in shape, spacing, type and device, are wanted")
+    (N, K), gated = W.shape, 0 if up is None else 1
+    code = _dtype_code(W.dtype)
+    with torch.cuda.device(W.device):
+        codes = torch.empty(max(lib().slicemoe_mx4_codes_bytes(N, K, gated), 1), dtype=torch.uint8, device=W.device)
+        scale = torch.empty(max(lib().slicemoe_mx4_scale_bytes(N, K, gated), 1), dtype=torch.uint8, device=W.device)
+        _check(lib().slicemoe_mx4_pack(_ptr(W), _ptr(up), code, N, K, W.stride(0), _ptr(codes), _ptr(scale), _stream(stream)),
+               "slicemoe_mx4_pack")
+    return Mx4Mat(N, K, gated, codes, scale)
+
+
+def slicemoe_mx4_unpack(mat: Mx4Mat, part: int = 0, stream=None):
+    """(codes [N, K / 2], scale [N, pitch]) of a packed matrix, or of gate (part 0) or up (part 1), as slicemoe_mx4_quantize returns them."""
+    import torch
+    dev = mat.codes.device
+    with torch.cuda.device(dev):
+        codes = torch.empty((mat.N, mat.K // 2), dtype=torch.uint8, device=dev)
+        scale = torch.empty((mat.N, lib().slicemoe_mx4_scale_pitch(mat.K)), dtype=torch.uint8, device=dev)
+        _check(lib().slicemoe_mx4_unpack(_ptr(mat.codes), _ptr(mat.scale), mat.N, mat.K, 1 if mat.gated else 0, part, _ptr(codes),
+                                         _ptr(scale), _stream(stream)), "slicemoe_mx4_unpack")
+    return codes, scale
+
+
+class Mx4Table:
+    """The device array of slicemoe_mx4_mat of a layer's experts; keeps the matrices alive."""
+
+    def __init__(self, mats, device):
+        import torch
+        self.mats = list(mats)
+        first = self.mats[0]
+        if any((m.N, m.K, m.gated) != (first.N, first.K, first.gated) for m in self.mats):
+            raise ValueError("matrices of one size and kind are wanted")
+        self.N, self.K, self.gated, self.n_experts = first.N, first.K, first.gated, len(self.mats)
+        arr = (Mx4MatDesc * len(self.mats))(*[m.desc() for m in self.mats])
+        self.device_array = torch.frombuffer(bytearray(bytes(arr)), dtype=torch.uint8).to(device)
+
+
+def mx4_table(mats, device=None) -> Mx4Table:
+    mats = list(mats)
+    return Mx4Table(mats, mats[0].codes.device if device is None else device)
+
+
+def slicemoe_mx4_workspace_bytes(T: int, k: int, n_experts: int) -> int:
+    return int(lib().slicemoe_mx4_workspace_bytes(T, k, n_experts))
+
+
+def new_mx4_workspace(T: int, k: int, n_experts: int, device="cuda", stream=None):
+    """For calls of up to T tokens with k experts each, of up to n_experts."""
+    import torch
+    nbytes = slicemoe_mx4_workspace_bytes(T, k, n_experts)
+    if nbytes == 0:
+        raise SliceMoEError(E_INVALID_ARG, "slicemoe_mx4_workspace_bytes")
+    with torch.cuda.device(device):
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        _check(lib().slicemoe_mx4_workspace_init(_ptr(ws), nbytes, _stream(stream)), "slicemoe_mx4_workspace_init")
+    return ws
+
+
+def slicemoe_mx4_product(table: Mx4Table, codes, scale, ids, ws, dtype=None, out=None, stream=None):
+    """codes, scale: [T, K / 2], or [T, k, K / 2] for a row per pair; ids: int32 [T, k] -> out [T, k, N] of `dtype` (or of `out`).
+    ids None: every row times the table's first matrix -> [T, N]."""
+    return (_m or _marshal()).mx4_product(table.device_array, table.n_experts, table.N, table.K, table.gated, codes, scale, ids, ws, dtype,
+                                          out, stream)
+
+
+def slicemoe_combine(rows, weights, ids=None, n_experts: int = 0, base=None, dtype=None, out=None, stream=None):
+    """rows [T, k, N], weights float32 [T, k] -> base + the weighted sum, [T, N] of `dtype` (or of `out`).  With ids, pairs whose id is
+    outside [0, n_experts) are left out."""
+    return (_m or _marshal()).combine(rows, weights, ids, n_experts, base, dtype, out, stream)
+
+
+def mx4_expert_ffn(gate_up: Mx4Table, down: Mx4Table, x, ids, weights, ws, base=None, dtype=None, stream=None):
+    """The expert FFN of one layer with weights in microscaled 4-bit floats: x [T, hidden], ids / weights [T, k] as
+    slicemoe_route_scored returns them -> base + sum_j weights[t, j] down_e(silu(gate_e x) * (up_e x)), [T, hidden] of `dtype` (x's).
+    Activations are quantised before either product; between them they are bf16.  A pair whose id names no expert adds nothing."""
+    import torch
+    with torch.cuda.stream(stream):   # what lies between the calls belongs to the stream that uses it
+        h = slicemoe_mx4_product(gate_up, *slicemoe_mx4_quantize(x), ids, ws, dtype=torch.bfloat16)
+        y = slicemoe_mx4_product(down, *slicemoe_mx4_quantize(h), ids, ws, dtype=torch.bfloat16)
+        return slicemoe_combine(y, weights, ids, min(gate_up.n_experts, down.n_experts), base, dtype or x.dtype)
 
 
 # ---- host DBSC -------------------------------------------------------------------------------------

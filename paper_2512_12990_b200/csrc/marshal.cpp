@@ -14,6 +14,7 @@
 #include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -36,6 +37,12 @@ struct Entry {
   decltype(&slicemoe_decode_step_host) decode_step_host;
   decltype(&slicemoe_prefill_layer) prefill_layer;
   decltype(&slicemoe_dbsc_assign) dbsc_assign;
+  decltype(&slicemoe_route_scored) route_scored;
+  decltype(&slicemoe_mx4_scale_pitch) mx4_scale_pitch;
+  decltype(&slicemoe_mx4_quantize) mx4_quantize;
+  decltype(&slicemoe_mx4_dequantize) mx4_dequantize;
+  decltype(&slicemoe_mx4_product) mx4_product;
+  decltype(&slicemoe_combine) combine;
 } lib;
 PyObject* error_type = nullptr;  // binding.SliceMoEError(code, where)
 PyObject* s_data_ptr = nullptr;
@@ -227,6 +234,12 @@ PyObject* py_setup(SM_ARGS) {  // (error type, dict name -> address)
     load("slicemoe_decode_step_host", lib.decode_step_host);
     load("slicemoe_prefill_layer", lib.prefill_layer);
     load("slicemoe_dbsc_assign", lib.dbsc_assign);
+    load("slicemoe_route_scored", lib.route_scored);
+    load("slicemoe_mx4_scale_pitch", lib.mx4_scale_pitch);
+    load("slicemoe_mx4_quantize", lib.mx4_quantize);
+    load("slicemoe_mx4_dequantize", lib.mx4_dequantize);
+    load("slicemoe_mx4_product", lib.mx4_product);
+    load("slicemoe_combine", lib.combine);
     Py_XSETREF(error_type, Py_NewRef(a[0]));
     Py_RETURN_NONE;
   });
@@ -521,11 +534,272 @@ PyObject* py_prefill_layer(SM_ARGS) {
   });
 }
 
+// ---- microscaled 4-bit floats and the routing that goes with them: tensors are looked at more closely than above, since a wrong
+// one would be read as bytes ----
+[[noreturn]] void refuse(const char* what) {
+  PyErr_SetString(PyExc_ValueError, what);
+  throw Failed();
+}
+int dtype_of(at::ScalarType t) {
+  if (t == at::kFloat) return SLICEMOE_F32;
+  if (t == at::kBFloat16) return SLICEMOE_BF16;
+  if (t == at::kHalf) return SLICEMOE_F16;
+  refuse("float32, bfloat16 or float16 is wanted");
+}
+at::ScalarType dtype_arg(PyObject* o) {
+  if (!THPDtype_Check(o)) refuse("dtype: a torch.dtype is wanted");
+  const at::ScalarType t = reinterpret_cast<THPDtype*>(o)->scalar_type;
+  dtype_of(t);
+  return t;
+}
+int int_of(int64_t v) {
+  if (v > INT32_MAX) refuse("a size is too large");
+  return (int)v;
+}
+// A CUDA tensor on the given device (an undefined device: any) of one type, contiguous.
+const at::Tensor& plain(PyObject* o, const char* name, at::ScalarType type, const at::Device* dev) {
+  const at::Tensor& t = tensor(o, name);
+  if (!t.is_cuda() || t.scalar_type() != type || !t.is_contiguous() || (dev && t.device() != *dev)) {
+    PyErr_Format(PyExc_ValueError, "%s: a contiguous CUDA tensor of the right type on the inputs' device is wanted", name);
+    throw Failed();
+  }
+  return t;
+}
+// A matrix (or stack of them) whose rows are evenly spaced: the last dimension dense, the others as if it were padded.
+struct Rows {
+  const void* at;
+  int64_t rows, cols, ld;
+  int dtype;
+  Rows(const at::Tensor& t, const char* name) {
+    bool ok = t.is_cuda() && t.dim() >= 1 && (t.size(-1) <= 1 || t.stride(-1) == 1);
+    at = t.const_data_ptr();
+    dtype = dtype_of(t.scalar_type());
+    cols = t.dim() ? t.size(-1) : 0;
+    rows = 1;
+    ld = cols;
+    bool first = true;
+    for (int64_t d = t.dim() - 2; d >= 0; --d) {
+      if (t.size(d) == 1) continue;
+      if (first)
+        ld = t.stride(d);
+      else
+        ok = ok && t.stride(d) == ld * rows;
+      first = false;
+      rows *= t.size(d);
+    }
+    if (!ok) {
+      PyErr_Format(PyExc_ValueError, "%s: a CUDA tensor with dense, evenly spaced rows is wanted", name);
+      throw Failed();
+    }
+  }
+};
+// The library launches on the device that is current: that of the tensors.
+class OnDevice {
+ public:
+  explicit OnDevice(at::Device d) : guard_(d) {}
+
+ private:
+  c10::cuda::OptionalCUDAGuard guard_;
+};
+
+// logits, k, score, bias, n_group, topk_group, group_best, renorm, scale, tau, rank_high, want_prec, stream -> (ids, weights, prec)
+PyObject* py_route_scored(SM_ARGS) {
+  return guarded([&]() -> PyObject* {
+    want(n, 13);
+    const at::Tensor& logits = tensor(a[0], "logits");
+    if (!logits.is_cuda() || logits.dim() != 2) refuse("logits: a CUDA matrix is wanted");
+    const at::Device dev = logits.device();
+    const OnDevice guard(dev);
+    const Rows x(logits, "logits");
+    const int k = integer32(a[1]), score = integer32(a[2]);
+    const float* bias = nullptr;
+    if (a[3] != Py_None) {
+      const at::Tensor& b = plain(a[3], "bias", at::kFloat, &dev);
+      if (b.numel() != x.cols) refuse("bias: one value per expert is wanted");
+      bias = static_cast<const float*>(b.const_data_ptr());
+    }
+    const int n_group = integer32(a[4]), topk_group = integer32(a[5]), best = integer32(a[6]), renorm = truth(a[7]);
+    const float scale = real(a[8]), tau = real(a[9]);
+    const int rank_high = integer32(a[10]), T = int_of(logits.size(0)), E = int_of(x.cols), kk = std::max(k, 1);
+    at::Tensor ids, w, prec;
+    const bool want_prec = truth(a[11]);
+    {
+      const Outputs out(dev);
+      ids = out({T, kk}, at::kInt), w = out({T, kk}, at::kFloat);
+      if (want_prec) prec = out({T, kk}, at::kByte);
+    }
+    void* st = stream_of(a[12]);
+    check(unlocked([&] {
+            return lib.route_scored(x.at, x.dtype, T, E, std::max(x.ld, x.cols), score, bias, n_group, topk_group, best, k, renorm, scale, tau,
+                                    rank_high, static_cast<int32_t*>(ids.data_ptr()), static_cast<float*>(w.data_ptr()),
+                                    prec.defined() ? static_cast<uint8_t*>(prec.data_ptr()) : nullptr, st);
+          }),
+          "slicemoe_route_scored");
+    return tuple_of({&ids, &w, &prec});
+  });
+}
+
+PyObject* py_mx4_quantize(SM_ARGS) {  // x, stream -> (codes, scale)
+  return guarded([&]() -> PyObject* {
+    want(n, 2);
+    const at::Tensor& x = tensor(a[0], "x");
+    const Rows r(x, "x");
+    const at::Device dev = x.device();
+    const OnDevice guard(dev);
+    const int rows = int_of(r.rows), K = int_of(r.cols);
+    auto sizes = x.sizes().vec();
+    at::Tensor codes, scale;
+    {
+      const Outputs out(dev);
+      sizes.back() = K / 2;
+      codes = out(sizes, at::kByte);
+      sizes.back() = (int64_t)lib.mx4_scale_pitch(K);
+      scale = out(sizes, at::kByte);
+    }
+    void* st = stream_of(a[1]);
+    check(unlocked([&] {
+            return lib.mx4_quantize(r.at, r.dtype, rows, K, r.ld, static_cast<uint8_t*>(codes.data_ptr()), static_cast<uint8_t*>(scale.data_ptr()), st);
+          }),
+          "slicemoe_mx4_quantize");
+    return tuple_of({&codes, &scale});
+  });
+}
+
+// Codes and scales that belong together: [..., K / 2] and [..., pitch]; rows and K.
+void mx4_rows(const at::Tensor& codes, const at::Tensor& scale, int* rows, int* K) {
+  if (codes.dim() < 1 || codes.dim() != scale.dim()) refuse("codes and scale: as slicemoe_mx4_quantize returns them");
+  for (int64_t d = 0; d + 1 < codes.dim(); ++d)
+    if (codes.size(d) != scale.size(d)) refuse("codes and scale: the same rows are wanted");
+  *K = int_of(2 * codes.size(-1));
+  if (scale.size(-1) != (int64_t)lib.mx4_scale_pitch(*K)) refuse("scale: slicemoe_mx4_scale_pitch(K) bytes per row are wanted");
+  *rows = int_of(codes.size(-1) ? codes.numel() / codes.size(-1) : 0);
+}
+
+PyObject* py_mx4_dequantize(SM_ARGS) {  // codes, scale, dtype, out, stream -> out
+  return guarded([&]() -> PyObject* {
+    want(n, 5);
+    const at::Tensor& codes = plain(a[0], "codes", at::kByte, nullptr);
+    const at::Device dev = codes.device();
+    const at::Tensor& scale = plain(a[1], "scale", at::kByte, &dev);
+    const OnDevice guard(dev);
+    int rows, K;
+    mx4_rows(codes, scale, &rows, &K);
+    auto sizes = codes.sizes().vec();
+    sizes.back() = K;
+    at::Tensor made;
+    const at::Tensor* out = &made;
+    if (a[3] != Py_None) {
+      out = &tensor(a[3], "out");
+      if (out->device() != dev || out->sizes() != at::IntArrayRef(sizes)) refuse("out: another shape or device");
+    } else {
+      made = Outputs(dev)(sizes, dtype_arg(a[2]));
+    }
+    const Rows r(*out, "out");
+    void* st = stream_of(a[4]);
+    check(unlocked([&] {
+            return lib.mx4_dequantize(static_cast<const uint8_t*>(codes.const_data_ptr()), static_cast<const uint8_t*>(scale.const_data_ptr()), rows, K,
+                                      const_cast<void*>(r.at), r.dtype, r.ld, st);
+          }),
+          "slicemoe_mx4_dequantize");
+    return a[3] != Py_None ? Py_NewRef(a[3]) : wrap(made);
+  });
+}
+
+// mats, n_experts, N, K, gated, codes, scale, ids, ws, dtype, out, stream -> out
+PyObject* py_mx4_product(SM_ARGS) {
+  return guarded([&]() -> PyObject* {
+    want(n, 12);
+    const at::Tensor& codes = plain(a[5], "codes", at::kByte, nullptr);
+    const at::Device dev = codes.device();
+    const at::Tensor &scale = plain(a[6], "scale", at::kByte, &dev), &mats = plain(a[0], "mats", at::kByte, &dev), &ws = plain(a[8], "ws", at::kByte, &dev);
+    const OnDevice guard(dev);
+    const int E = integer32(a[1]), N = integer32(a[2]), K = integer32(a[3]), gated = truth(a[4]);
+    if (mats.numel() < (int64_t)sizeof(slicemoe_mx4_mat) * E) refuse("mats: fewer matrices than n_experts");
+    int rows, k_x;
+    mx4_rows(codes, scale, &rows, &k_x);
+    if (k_x != K) refuse("codes: their width is not that of the matrices");
+    int T = rows, k = 1, per_pair = 0;
+    const int32_t* ids = nullptr;
+    if (a[7] != Py_None) {
+      const at::Tensor& t = plain(a[7], "ids", at::kInt, &dev);
+      if (t.dim() != 2) refuse("ids: [tokens, k] is wanted");
+      T = int_of(t.size(0)), k = int_of(t.size(1));
+      per_pair = codes.dim() == 3;
+      if (per_pair ? codes.size(0) != T || codes.size(1) != k : codes.dim() != 2 || codes.size(0) != T) refuse("codes: [tokens, K / 2] or [tokens, k, K / 2] is wanted");
+      ids = static_cast<const int32_t*>(t.const_data_ptr());
+    } else if (codes.dim() != 2) {
+      refuse("codes: [rows, K / 2] is wanted");
+    }
+    at::Tensor made;
+    const at::Tensor* out = &made;
+    const std::initializer_list<int64_t> three = {T, k, N}, two = {T, N};
+    const at::IntArrayRef sizes = ids ? at::IntArrayRef(three) : at::IntArrayRef(two);
+    if (a[10] != Py_None) {
+      out = &tensor(a[10], "out");
+      if (out->device() != dev || out->sizes() != sizes || !out->is_contiguous()) refuse("out: another shape or device, or not contiguous");
+    } else {
+      made = Outputs(dev)(sizes, dtype_arg(a[9]));
+    }
+    const int dtype = dtype_of(out->scalar_type());
+    void* st = stream_of(a[11]);
+    check(unlocked([&] {
+            return lib.mx4_product(static_cast<const slicemoe_mx4_mat*>(mats.const_data_ptr()), E, N, K, gated, static_cast<const uint8_t*>(codes.const_data_ptr()),
+                                   static_cast<const uint8_t*>(scale.const_data_ptr()), T, k, per_pair, ids, out->data_ptr(), dtype, ws.data_ptr(),
+                                   (size_t)ws.numel(), st);
+          }),
+          "slicemoe_mx4_product");
+    return a[10] != Py_None ? Py_NewRef(a[10]) : wrap(made);
+  });
+}
+
+PyObject* py_combine(SM_ARGS) {  // rows, weights, ids, n_experts, base, dtype, out, stream -> out
+  return guarded([&]() -> PyObject* {
+    want(n, 8);
+    const at::Tensor& rows = tensor(a[0], "rows");
+    if (!rows.is_cuda() || rows.dim() != 3 || !rows.is_contiguous()) refuse("rows: a contiguous CUDA tensor [tokens, k, N] is wanted");
+    const at::Device dev = rows.device();
+    const OnDevice guard(dev);
+    const int T = int_of(rows.size(0)), k = int_of(rows.size(1)), N = int_of(rows.size(2));
+    const at::Tensor& w = plain(a[1], "weights", at::kFloat, &dev);
+    if (w.numel() != (int64_t)T * k) refuse("weights: [tokens, k] is wanted");
+    const int32_t* ids = nullptr;
+    int n_experts = 0;
+    if (a[2] != Py_None) {
+      const at::Tensor& t = plain(a[2], "ids", at::kInt, &dev);
+      if (t.numel() != (int64_t)T * k) refuse("ids: [tokens, k] is wanted");
+      ids = static_cast<const int32_t*>(t.const_data_ptr());
+      n_experts = integer32(a[3]);
+    }
+    at::Tensor made;
+    const at::Tensor* out = &made;
+    if (a[6] != Py_None) {
+      out = &tensor(a[6], "out");
+      if (out->device() != dev || out->numel() != (int64_t)T * N || !out->is_contiguous()) refuse("out: another shape or device, or not contiguous");
+    } else {
+      made = Outputs(dev)({T, N}, dtype_arg(a[5]));
+    }
+    const void* base = nullptr;
+    if (a[4] != Py_None) {
+      const at::Tensor& b = plain(a[4], "base", out->scalar_type(), &dev);
+      if (b.numel() != (int64_t)T * N) refuse("base: [tokens, N] is wanted");
+      base = b.const_data_ptr();
+    }
+    const int rd = dtype_of(rows.scalar_type()), od = dtype_of(out->scalar_type());
+    void* st = stream_of(a[7]);
+    check(unlocked([&] {
+            return lib.combine(rows.const_data_ptr(), rd, T, k, N, static_cast<const float*>(w.const_data_ptr()), ids, n_experts, base, out->data_ptr(), od, st);
+          }),
+          "slicemoe_combine");
+    return a[6] != Py_None ? Py_NewRef(a[6]) : wrap(made);
+  });
+}
+
 #define SM_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_##name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {SM_METHOD(setup),        SM_METHOD(pack),         SM_METHOD(route_topk),
                          SM_METHOD(expert_ffn),   SM_METHOD(layer),            SM_METHOD(layer_static),
                          SM_METHOD(layer_routed), SM_METHOD(decode_step_host), SM_METHOD(prefill_layer),
-                         SM_METHOD(dbsc_assign),
+                         SM_METHOD(dbsc_assign),  SM_METHOD(route_scored),     SM_METHOD(mx4_quantize),
+                         SM_METHOD(mx4_dequantize), SM_METHOD(mx4_product),    SM_METHOD(combine),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

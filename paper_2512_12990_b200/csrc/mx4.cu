@@ -1,0 +1,213 @@
+// slicemoe_mx4_quantize / _dequantize / _pack / _unpack: values to microscaled 4-bit floats and back.
+#include "mx4.cuh"
+
+namespace slicemoe {
+
+constexpr int kMxThreads = 256;
+
+// Four lanes hold a block of 32 values, eight each: the largest magnitude by two exchanges, then each lane writes the four bytes
+// of its eight codes (a warp's stores are 128 consecutive bytes) and the first the scale.  Bound: the values read.
+template <class T, bool WIDE>
+__global__ void __launch_bounds__(kMxThreads) mx_quantize_kernel(const T* __restrict__ x, int rows, int K, int64_t ld,
+                                                                 uint8_t* __restrict__ codes, uint8_t* __restrict__ scale) {
+  mx_dep_launch();
+  mx_dep_wait();
+  const int per_row = K >> 3, pitch = mx_pitch(K), blocks = K / kMxBlock;
+  const int64_t n = (int64_t)rows * per_row;
+  const int64_t step = (int64_t)gridDim.x * kMxThreads;
+  // the four lanes of a block take part together: n is a multiple of 4
+  for (int64_t i = (int64_t)blockIdx.x * kMxThreads + threadIdx.x; i < n; i += step) {
+    const int64_t row = i / per_row;
+    const int c = (int)(i - row * per_row);
+    float v[8];
+    mx_load8<T, WIDE>(x + row * ld + 8 * c, v);
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(v[j]) & 0x7fffffffu);
+    const unsigned quad = 0xfu << (threadIdx.x & 28);
+    m = max(m, __shfl_xor_sync(quad, m, 1));
+    m = max(m, __shfl_xor_sync(quad, m, 2));
+    const uint32_t b = mx_scale_byte(m);
+    if (b == 255u) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+    }
+    *reinterpret_cast<uint32_t*>(codes + row * (K >> 1) + 4 * c) = mx_encode8(v, mx_inverse(b));
+    if ((c & 3) == 0) {
+      const int kb = c >> 2;
+      uint8_t* s = scale + row * pitch + kb;
+      *s = (uint8_t)b;
+      if (kb == blocks - 1)
+        for (int p = blocks; p < pitch; ++p) scale[row * pitch + p] = 0;
+    }
+  }
+}
+
+template <class T, bool WIDE>
+__global__ void __launch_bounds__(kMxThreads) mx_dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scale,
+                                                                   int rows, int K, T* __restrict__ out, int64_t ld) {
+  mx_dep_launch();
+  mx_dep_wait();
+  const int per_row = K >> 3, pitch = mx_pitch(K);
+  const int64_t n = (int64_t)rows * per_row;
+  const int64_t step = (int64_t)gridDim.x * kMxThreads;
+  for (int64_t i = (int64_t)blockIdx.x * kMxThreads + threadIdx.x; i < n; i += step) {
+    const int64_t row = i / per_row;
+    const int c = (int)(i - row * per_row);
+    const uint32_t w = __ldcg(reinterpret_cast<const uint32_t*>(codes + row * (K >> 1)) + c);
+    const float s = mx_scale_value(__ldcg(scale + row * pitch + (c >> 2)));
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 f = __half22float2(mx_decode2(w >> (8 * j)));
+      v[2 * j] = f.x * s;
+      v[2 * j + 1] = f.y * s;
+    }
+    mx_store8<T, WIDE>(out + row * ld + 8 * c, v);
+  }
+}
+
+// Pack: a thread per block of 32 values of a physical row, eight rows x four blocks a warp, so that reads are whole sectors and
+// writes 128 consecutive bytes.  Rows and blocks beyond the matrix are written as zeros.
+template <class T>
+__global__ void __launch_bounds__(kMxThreads) mx_pack_kernel(const T* __restrict__ W, const T* __restrict__ up, int N, int K, int64_t ld,
+                                                             uint8_t* __restrict__ codes, uint8_t* __restrict__ scale) {
+  const int gated = up != nullptr;
+  const int row = blockIdx.y * kMxRows + (threadIdx.x >> 5) * 8 + (threadIdx.x & 7);  // 8 warps: 64 rows; twice
+  const int kb = blockIdx.x * 4 + ((threadIdx.x & 31) >> 3);
+#pragma unroll 1
+  for (int half = 0; half < 2; ++half) {
+    const int r = row + half * 64;
+    const T* src = W;
+    int n = r;
+    if (gated) {
+      n = (r >> 5) * 16 + (r & 15);
+      if (r & 16) src = up;
+    }
+    uint32_t w[4] = {0, 0, 0, 0}, b = 0;
+    if (n < N && kb * kMxBlock < K) {
+      const T* p = src + n * ld + (int64_t)kb * kMxBlock;
+      float v[32];
+#pragma unroll
+      for (int j = 0; j < 32; ++j) v[j] = mx_to_float<T>(p[j]);
+      uint32_t m = 0;
+#pragma unroll
+      for (int j = 0; j < 32; ++j) m = max(m, __float_as_uint(v[j]) & 0x7fffffffu);
+      b = mx_scale_byte(m);
+      const float inv = mx_inverse(b);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float e[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e[j] = b == 255u ? 0.0f : v[8 * q + j];
+        w[q] = mx_encode8(e, inv);
+      }
+    }
+    if ((kb >> 1) < mx_chunks(K)) *reinterpret_cast<uint4*>(codes + mx_code_offset(K, r, kb)) = make_uint4(w[0], w[1], w[2], w[3]);
+    scale[mx_scale_offset(K, r, kb)] = (uint8_t)b;
+  }
+}
+
+__global__ void __launch_bounds__(kMxThreads) mx_unpack_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scale, int N, int K,
+                                                               int gated, int part, uint8_t* __restrict__ codes_rm, uint8_t* __restrict__ scale_rm) {
+  const int blocks = K / kMxBlock, pitch = mx_pitch(K);
+  const int64_t n = (int64_t)N * pitch;
+  for (int64_t i = (int64_t)blockIdx.x * kMxThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kMxThreads) {
+    const int row = (int)(i / pitch), kb = (int)(i % pitch);
+    const int r = gated ? (row >> 4) * 32 + (row & 15) + 16 * part : row;
+    uint8_t b = 0;
+    if (kb < blocks) {
+      b = scale[mx_scale_offset(K, r, kb)];
+      *reinterpret_cast<uint4*>(codes_rm + (int64_t)row * (K >> 1) + 16 * kb) = *reinterpret_cast<const uint4*>(codes + mx_code_offset(K, r, kb));
+    }
+    scale_rm[i] = b;
+  }
+}
+
+static int mx_grid(int64_t threads) {
+  const int64_t b = (threads + kMxThreads - 1) / kMxThreads;
+  return (int)(b < 148 * 64 ? b : 148 * 64);
+}
+
+template <class T>
+static int quantize_as(const void* x, int rows, int K, int64_t ld, uint8_t* codes, uint8_t* scale, cudaStream_t st) {
+  const bool wide = mx_aligned(x, 16) && (ld * sizeof(T)) % 16 == 0;
+  return mx_launch(wide ? mx_quantize_kernel<T, true> : mx_quantize_kernel<T, false>, dim3(mx_grid((int64_t)rows * (K >> 3))), kMxThreads, 0, st,
+                   static_cast<const T*>(x), rows, K, ld, codes, scale);
+}
+template <class T>
+static int dequantize_as(const uint8_t* codes, const uint8_t* scale, int rows, int K, void* out, int64_t ld, cudaStream_t st) {
+  const bool wide = mx_aligned(out, 16) && (ld * sizeof(T)) % 16 == 0;
+  return mx_launch(wide ? mx_dequantize_kernel<T, true> : mx_dequantize_kernel<T, false>, dim3(mx_grid((int64_t)rows * (K >> 3))), kMxThreads, 0,
+                   st, codes, scale, rows, K, static_cast<T*>(out), ld);
+}
+
+static int mx_check(const void* x, int dtype, int rows, int K, int64_t ld, const void* codes, const void* scale) {
+  if (!x || !codes || !scale || rows <= 0 || K <= 0 || K % kMxBlock || ld < K) return SLICEMOE_E_INVALID_ARG;
+  if (!mx_dtype(dtype)) return SLICEMOE_E_UNSUPPORTED;
+  if (!mx_aligned(x, mx_elem(dtype)) || !mx_aligned(codes, 16) || !mx_aligned(scale, 4)) return SLICEMOE_E_INVALID_ARG;
+  return SLICEMOE_OK;
+}
+
+}  // namespace slicemoe
+
+using namespace slicemoe;
+
+extern "C" size_t slicemoe_mx4_scale_pitch(int K) { return K > 0 ? (size_t)mx_pitch(K) : 0; }
+
+extern "C" int slicemoe_mx4_quantize(const void* x, int dtype, int rows, int K, int64_t ld, uint8_t* codes, uint8_t* scale, void* stream) {
+  const int rc = mx_check(x, dtype, rows, K, ld, codes, scale);
+  if (rc != SLICEMOE_OK) return rc;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (dtype == SLICEMOE_F32) return quantize_as<float>(x, rows, K, ld, codes, scale, st);
+  if (dtype == SLICEMOE_BF16) return quantize_as<__nv_bfloat16>(x, rows, K, ld, codes, scale, st);
+  return quantize_as<__half>(x, rows, K, ld, codes, scale, st);
+}
+
+extern "C" int slicemoe_mx4_dequantize(const uint8_t* codes, const uint8_t* scale, int rows, int K, void* out, int dtype, int64_t ld, void* stream) {
+  const int rc = mx_check(out, dtype, rows, K, ld, codes, scale);
+  if (rc != SLICEMOE_OK) return rc;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (dtype == SLICEMOE_F32) return dequantize_as<float>(codes, scale, rows, K, out, ld, st);
+  if (dtype == SLICEMOE_BF16) return dequantize_as<__nv_bfloat16>(codes, scale, rows, K, out, ld, st);
+  return dequantize_as<__half>(codes, scale, rows, K, out, ld, st);
+}
+
+static bool mx_sizes(int N, int K) { return N > 0 && K > 0 && K % kMxBlock == 0 && N <= kMxMaxN && K <= kMxMaxK; }
+
+extern "C" size_t slicemoe_mx4_codes_bytes(int N, int K, int gated) {
+  return mx_sizes(N, K) ? (size_t)mx_row_blocks(N, gated) * mx_chunks(K) * kMxChunkBytes : 0;
+}
+extern "C" size_t slicemoe_mx4_scale_bytes(int N, int K, int gated) {
+  return mx_sizes(N, K) ? (size_t)mx_row_blocks(N, gated) * mx_atoms(K) * kMxAtomBytes : 0;
+}
+
+extern "C" int slicemoe_mx4_pack(const void* W, const void* up, int dtype, int N, int K, int64_t ld, uint8_t* codes, uint8_t* scale, void* stream) {
+  const int rc = mx_check(W, dtype, N, K, ld, codes, scale);
+  if (rc != SLICEMOE_OK) return rc;
+  if (up && !mx_aligned(up, mx_elem(dtype))) return SLICEMOE_E_INVALID_ARG;
+  if (!mx_aligned(scale, 16)) return SLICEMOE_E_INVALID_ARG;
+  if (!mx_sizes(N, K)) return SLICEMOE_E_UNSUPPORTED;
+  const dim3 grid(mx_atoms(K), mx_row_blocks(N, up != nullptr));
+  if (grid.y > 65535u) return SLICEMOE_E_UNSUPPORTED;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (dtype == SLICEMOE_F32)
+    mx_pack_kernel<float><<<grid, kMxThreads, 0, st>>>(static_cast<const float*>(W), static_cast<const float*>(up), N, K, ld, codes, scale);
+  else if (dtype == SLICEMOE_BF16)
+    mx_pack_kernel<__nv_bfloat16><<<grid, kMxThreads, 0, st>>>(static_cast<const __nv_bfloat16*>(W), static_cast<const __nv_bfloat16*>(up), N, K, ld,
+                                                               codes, scale);
+  else
+    mx_pack_kernel<__half><<<grid, kMxThreads, 0, st>>>(static_cast<const __half*>(W), static_cast<const __half*>(up), N, K, ld, codes, scale);
+  SM_LAUNCH_CHECK();
+  return SLICEMOE_OK;
+}
+
+extern "C" int slicemoe_mx4_unpack(const uint8_t* codes, const uint8_t* scale, int N, int K, int gated, int part, uint8_t* codes_rm,
+                                   uint8_t* scale_rm, void* stream) {
+  if (!codes || !scale || !codes_rm || !scale_rm || N <= 0 || K <= 0 || K % kMxBlock || part < 0 || part > (gated ? 1 : 0)) return SLICEMOE_E_INVALID_ARG;
+  if (!mx_aligned(codes, 16) || !mx_aligned(codes_rm, 16)) return SLICEMOE_E_INVALID_ARG;
+  if (!mx_sizes(N, K)) return SLICEMOE_E_UNSUPPORTED;
+  mx_unpack_kernel<<<mx_grid((int64_t)N * mx_pitch(K)), kMxThreads, 0, (cudaStream_t)stream>>>(codes, scale, N, K, gated, part, codes_rm, scale_rm);
+  SM_LAUNCH_CHECK();
+  return SLICEMOE_OK;
+}
