@@ -385,3 +385,33 @@ def test_a_layer_from_logits_to_output(T):
     g.replay()
     assert torch.equal(again, out)
     assert B.slicemoe_get_status(ws) == 0
+
+
+@pytest.mark.parametrize("T,k,E,N,K,dtype", [(700, 2, 3, 1920, 1408, "f32"), (2048, 4, 60, 704, 2048, "bf16"), (3000, 6, 64, 512, 1056, "f32")])
+def test_long_prompts_agree_with_single_rows(T, k, E, N, K, dtype):
+    """Many items to a CTA, rings that go round often: sampled rows against calls of one token, bit for bit, and against the
+    dequantised product in fp64."""
+    import torch
+    from paper_2512_12990_b200 import binding as B
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(T)
+    w = [torch.randn(2 * N, K, device="cuda", generator=gen) * 0.1 for _ in range(E)]
+    table = B.mx4_table([B.slicemoe_mx4_pack(m[:N], m[N:]) for m in w])
+    codes, scale = B.slicemoe_mx4_quantize(torch.randn(T, K, device="cuda", generator=gen))
+    ids = torch.rand(T, E, device="cuda", generator=gen).topk(k, -1).indices.int()
+    ws = B.new_mx4_workspace(T, k, E)
+    out = B.slicemoe_mx4_product(table, codes, scale, ids, ws, dtype=_dt(dtype))
+    assert B.slicemoe_get_status(ws) == 0
+    for t in range(0, T, T // 37):
+        one = B.slicemoe_mx4_product(table, codes[t:t + 1].contiguous(), scale[t:t + 1].contiguous(), ids[t:t + 1].contiguous(), ws, dtype=_dt(dtype))
+        assert torch.equal(one[0], out[t])
+    x = B.slicemoe_mx4_dequantize(codes, scale, torch.float32).double()
+    for e in range(0, E, max(1, E // 5)):
+        at = torch.nonzero(ids == e)
+        m = B.slicemoe_mx4_dequantize(*B.slicemoe_mx4_quantize(w[e]), torch.float32).double()
+        g, u = (x[at[:, 0]] @ m.T).split(N, 1)
+        mg, mu = (x[at[:, 0]].abs() @ m.abs().T).split(N, 1)
+        y = torch.nn.functional.silu(g) * u
+        tol = K * 2.0 ** -23 * (1.1 * u.abs() * mg + torch.nn.functional.silu(g).abs() * mu) + 2.0 ** -20 * y.abs()
+        tol = tol + torch.from_numpy(np.asarray(_half_step((y.abs() + tol).cpu().numpy(), dtype))).cuda()
+        assert ((out[at[:, 0], at[:, 1]].double() - y).abs() <= tol).all()

@@ -104,3 +104,24 @@ def test_a_short_limit_is_not_spent_on_the_launch_before():
     for _ in range(20):
         assert torch.equal(B.slicemoe_layer(shape, table, None, None, x, ids, prec, w, ws), want)
     assert B.slicemoe_get_status(ws) == 0
+
+
+@pytest.mark.parametrize("T", [2, 300])
+def test_the_product_of_microscaled_experts_gives_up_by_itself(T):
+    """The waits for weights that are never brought run out: the call returns, the status says so, and the workspace serves on once
+    the switch is off again."""
+    import torch
+    from paper_2512_12990_b200 import binding as B
+    E, k, N, K = 4, 2, 256, 1024
+    mats = [B.slicemoe_mx4_pack(torch.randn(N, K, device="cuda")) for _ in range(E)]
+    table, ws = B.mx4_table(mats), B.new_mx4_workspace(T, k, E)
+    codes, scale = B.slicemoe_mx4_quantize(torch.randn(T, K, device="cuda"))
+    ids = torch.randint(0, E, (T, k), device="cuda", dtype=torch.int32)
+    ref = B.slicemoe_mx4_product(table, codes, scale, ids, ws, dtype=torch.float32)
+    assert B.slicemoe_get_status(ws) == 0
+    B.slicemoe_workspace_set_wait(ws, 200000, 1)
+    B.slicemoe_mx4_product(table, codes, scale, ids, ws, dtype=torch.float32)
+    assert B.slicemoe_get_status(ws) == B.STATUS_WAIT_TIMEOUT
+    B.slicemoe_workspace_set_wait(ws, 0, 0)
+    assert torch.equal(B.slicemoe_mx4_product(table, codes, scale, ids, ws, dtype=torch.float32), ref)
+    assert B.slicemoe_get_status(ws) == 0
