@@ -480,15 +480,16 @@ int slicemoe_mx4_unpack(const uint8_t *codes, const uint8_t *scale, int N, int K
  *   out        device [T, k, N] of `dtype`, rounded once from fp32; aligned to 16 bytes.  The row of a pair whose id is outside
  *              [0, n_experts) is left as it was, and SLICEMOE_STATUS_BAD_EXPERT_ID is set; so it is where the expert's table entry is
  *              not an N x K matrix of this kind (null pointers, other sizes)
- *   workspace  device, slicemoe_mx4_workspace_bytes(T, k, n_experts) bytes, 256-byte aligned, prepared once by
+ *   workspace  device, slicemoe_mx4_workspace_bytes(T, k, n_experts, K) bytes, 256-byte aligned, prepared once by
  *              slicemoe_mx4_workspace_init.  slicemoe_get_status reads (and clears) its status word and
  *              slicemoe_workspace_set_wait sets its wait limit, as for slicemoe_workspace_init's.  It serves one stream at a
- *              time; two calls that may overlap, or two graphs that may run at once, need one each
+ *              time; two calls that may overlap, or two graphs that may run at once, need one each.  One for larger T, k, n_experts or
+ *              K serves smaller calls too.  It holds the token rows in the order of the experts: about T k K / 2 bytes
  * A row's result does not depend on the other rows of the call, bit for bit, and is reproducible.
  * Errors: INVALID_ARG (null, sizes, alignment, workspace too small), UNSUPPORTED (n_experts > 1024, T k > 2^24, N > 2^24,
  * K > 2^20, k > SLICEMOE_MAX_TOP_K, dtype), CUDA.
  */
-size_t slicemoe_mx4_workspace_bytes(int T, int k, int n_experts);
+size_t slicemoe_mx4_workspace_bytes(int T, int k, int n_experts, int K);
 int slicemoe_mx4_workspace_init(void *workspace, size_t workspace_bytes, void *stream);
 int slicemoe_mx4_product(const slicemoe_mx4_mat *mats, int n_experts, int N, int K, int gated, const uint8_t *codes,
                          const uint8_t *scale, int T, int k, int x_per_pair, const int32_t *ids, void *out, int dtype,

@@ -167,7 +167,7 @@ def lib() -> ctypes.CDLL:
     L.slicemoe_mx4_scale_pitch.argtypes = [c_int]
     L.slicemoe_mx4_codes_bytes.argtypes = [c_int, c_int, c_int]
     L.slicemoe_mx4_scale_bytes.argtypes = [c_int, c_int, c_int]
-    L.slicemoe_mx4_workspace_bytes.argtypes = [c_int, c_int, c_int]
+    L.slicemoe_mx4_workspace_bytes.argtypes = [c_int, c_int, c_int, c_int]
     L.slicemoe_mx4_quantize.argtypes = [c_void_p, c_int, c_int, c_int, c_int64, c_void_p, c_void_p, c_void_p]
     L.slicemoe_mx4_dequantize.argtypes = [c_void_p, c_void_p, c_int, c_int, c_void_p, c_int, c_int64, c_void_p]
     L.slicemoe_mx4_pack.argtypes = [c_void_p, c_void_p, c_int, c_int, c_int, c_int64, c_void_p, c_void_p, c_void_p]
@@ -472,14 +472,15 @@ def mx4_table(mats, device=None) -> Mx4Table:
     return Mx4Table(mats, mats[0].codes.device if device is None else device)
 
 
-def slicemoe_mx4_workspace_bytes(T: int, k: int, n_experts: int) -> int:
-    return int(lib().slicemoe_mx4_workspace_bytes(T, k, n_experts))
+def slicemoe_mx4_workspace_bytes(T: int, k: int, n_experts: int, K: int) -> int:
+    return int(lib().slicemoe_mx4_workspace_bytes(T, k, n_experts, K))
 
 
-def new_mx4_workspace(T: int, k: int, n_experts: int, device="cuda", stream=None):
-    """For calls of up to T tokens with k experts each, of up to n_experts."""
+def new_mx4_workspace(T: int, k: int, n_experts: int, K: int = 4096, device="cuda", stream=None):
+    """For calls of up to T tokens with k experts each, of up to n_experts, and rows of up to K values (4096: the widest hidden of the
+    layer calls)."""
     import torch
-    nbytes = slicemoe_mx4_workspace_bytes(T, k, n_experts)
+    nbytes = slicemoe_mx4_workspace_bytes(T, k, n_experts, K)
     if nbytes == 0:
         raise SliceMoEError(E_INVALID_ARG, "slicemoe_mx4_workspace_bytes")
     with torch.cuda.device(device):

@@ -23,29 +23,46 @@ struct MpHeader {
 };
 constexpr int kMpMaxExperts = 1024;
 constexpr int64_t kMpMaxPairs = 1 << 24;
-constexpr int kMpInline = 512;       // up to here every CTA sorts the pairs itself; above, a kernel before does
-constexpr int kMpSortPairs = 4096;   // pairs of a block of that kernel
-constexpr int kMpSortThreads = 1024;
+constexpr int kMpTile = 224;         // most tokens of a tile
+constexpr int kMpInline = 512;       // pairs up to which the product's CTAs sort them and gather the rows themselves
+constexpr int kMpSortPairs = 4096;   // above: pairs of a block of the kernel that ranks them
+constexpr int kMpSortThreads = 1024, kMpPlaceThreads = 256;
 
-// Workspace: header, rows before each expert, the pairs by expert; and the same of each block where there is more than one.
+// An expert's rows are cut into as few tiles as they fit, of equal size (a multiple of 16).
+struct MpTiles {
+  int n, each;
+};
+__host__ __device__ inline MpTiles mp_tiles(int rows, int tile) {
+  MpTiles t;
+  t.n = (rows + tile - 1) / tile;
+  t.each = t.n ? ((rows + t.n - 1) / t.n + 15) & ~15 : 0;
+  return t;
+}
+// An expert has at most T rows where no token names one twice: wider tiles would only take room from the ring.
+__host__ __device__ inline int mp_tile(int T) { return T >= kMpTile ? kMpTile : (T + 15) & ~15; }
+
+// Workspace: header; ranks of the pairs among the block's of their expert, and the blocks' counts; rows before each expert, the pairs by
+// expert; token rows in the operand layout.  Every part grows with each argument, so that a workspace serves smaller calls.
 struct MpLayout {
-  size_t first, list, block_first, block_list, total;
+  size_t rank, hist, first, list, scale, codes, total;
   int blocks;
 };
-__host__ __device__ inline MpLayout mp_layout(int64_t pairs, int E) {
+__host__ __device__ inline MpLayout mp_layout(int T, int k, int E, int K) {
   auto up = [](size_t v) { return (v + 255) & ~(size_t)255; };
+  const int64_t pairs = (int64_t)T * k, tiles = (pairs / kMpTile > k ? pairs / kMpTile : k) + (pairs < E ? pairs : E) + 1;
   MpLayout l;
   l.blocks = (int)((pairs + kMpSortPairs - 1) / kMpSortPairs);
-  const bool many = l.blocks > 1;
-  l.first = 256;
+  l.rank = 256;
+  l.hist = l.rank + up(pairs * sizeof(int));
+  l.first = l.hist + up((size_t)l.blocks * E * sizeof(int));
   l.list = l.first + up((E + 1) * sizeof(int));
-  l.block_first = l.list + up(pairs * sizeof(int));
-  l.block_list = l.block_first + (many ? up((size_t)l.blocks * (E + 1) * sizeof(int)) : 0);
-  l.total = l.block_list + (many ? up(pairs * sizeof(int)) : 0);
+  l.scale = l.list + up(pairs * sizeof(int));
+  l.codes = l.scale + up((size_t)tiles * 2 * mx_atoms(K) * kMxAtomBytes);
+  l.total = l.codes + up((size_t)(pairs + 16 * tiles) * mx_chunks(K) * (kMxChunk / 2));
   return l;
 }
 
-// ---- pairs by expert ----------------------------------------------------------------------------------------------
+// ---- pairs by expert, and their rows into tiles --------------------------------------------------------------------
 // Exclusive scan over the block of one value per thread; *total gets the sum.  s: one int per warp.
 template <int THREADS>
 __device__ __forceinline__ int mp_scan(int v, int* s, int* total) {
@@ -67,91 +84,125 @@ __device__ __forceinline__ int mp_scan(int v, int* s, int* total) {
 struct MpSortParams {
   const int32_t* ids;
   int pairs, E;
-  int* first;  // [block][E + 1]
-  int* list;   // [block][kMpSortPairs]
+  int* rank;
+  int* hist;  // [block][E]
   MpHeader* head;
 };
-// A block's pairs by expert: a pair's rank among the block's of its expert is what the counting atomic returns.  (The order within an
-// expert depends on the atomics' order; which column of a tile a pair gets does not enter its result.)
+// A pair's rank among the block's of its expert is what the counting atomic returns.  (It depends on the atomics' order; which column
+// of a tile a pair gets does not enter its result.)
 __global__ void __launch_bounds__(kMpSortThreads) mp_sort_kernel(const MpSortParams p) {
-  __shared__ int s_first[kMpMaxExperts + 1], s_sums[32];
+  __shared__ int s_count[kMpMaxExperts];
   mx_dep_launch();
   const int tid = threadIdx.x;
-  s_first[tid] = 0;
-  if (tid == 0) s_first[kMpMaxExperts] = 0;
+  s_count[tid] = 0;
   mx_dep_wait();
   __syncthreads();
-  const int base = blockIdx.x * kMpSortPairs;
   constexpr int kEach = kMpSortPairs / kMpSortThreads;
-  int e[kEach], rank[kEach];
+  const int base = blockIdx.x * kMpSortPairs + tid;
+  int e[kEach];
   bool bad = false;
 #pragma unroll
   for (int i = 0; i < kEach; ++i) {
-    const int at = base + i * kMpSortThreads + tid;
+    const int at = base + i * kMpSortThreads;
     e[i] = at < p.pairs ? __ldcg(p.ids + at) : -1;
     bad |= at < p.pairs && (unsigned)e[i] >= (unsigned)p.E;
   }
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) rank[i] = (unsigned)e[i] < (unsigned)p.E ? atomicAdd(&s_first[e[i]], 1) : 0;
+  for (int i = 0; i < kEach; ++i) {
+    const int at = base + i * kMpSortThreads;
+    if (at < p.pairs) p.rank[at] = (unsigned)e[i] < (unsigned)p.E ? atomicAdd(&s_count[e[i]], 1) : -1;
+  }
   __syncthreads();
-  int total;
-  const int before = mp_scan<kMpSortThreads>(s_first[tid], s_sums, &total);
-  s_first[tid] = before;
-  if (tid == 0) s_first[kMpMaxExperts] = total;
-  __syncthreads();
-  for (int i = tid; i <= p.E; i += kMpSortThreads) p.first[(size_t)blockIdx.x * (p.E + 1) + i] = s_first[i];
-#pragma unroll
-  for (int i = 0; i < kEach; ++i)
-    if ((unsigned)e[i] < (unsigned)p.E) p.list[base + s_first[e[i]] + rank[i]] = base + i * kMpSortThreads + tid;
+  if (tid < p.E) p.hist[(size_t)blockIdx.x * p.E + tid] = s_count[tid];
   if (bad) atomicOr(&p.head->status, (unsigned)SLICEMOE_STATUS_BAD_EXPERT_ID);
 }
 
-struct MpMergeParams {
-  const int *block_first, *block_list;
-  int blocks, E;
+struct MpPlaceParams {
+  const int32_t* ids;  // NULL: all of expert 0, in order
+  const int *rank, *hist;
+  const uint8_t *codes, *scale;
   int *first, *list;
+  uint8_t *t_codes, *t_scale;
+  int pairs, E, blocks, chunk, tile, k, x_per_pair, K;
 };
-// The blocks' lists one behind the other: block b moves its own, an expert's pairs behind those of the blocks before.
-__global__ void __launch_bounds__(kMpSortThreads) mp_merge_kernel(const MpMergeParams p) {
-  __shared__ int s_at[kMpMaxExperts], s_sums[32];
+// Each pair's row to its place in its tile, in the layout of the tensor instruction's operand: a tile's 16-byte pieces [piece][row],
+// its scales as those of packed weights.  A block takes `chunk` pairs of one block of ranks.
+__global__ void __launch_bounds__(kMpPlaceThreads) mp_place_kernel(const MpPlaceParams p) {
+  __shared__ int s_first[kMpMaxExperts], s_before[kMpMaxExperts], s_count[kMpMaxExperts], s_tile[kMpMaxExperts], s_row[kMpMaxExperts], s_sums[32];
   mx_dep_launch();
   mx_dep_wait();
-  const int tid = threadIdx.x, me = blockIdx.x;
-  int count = 0, before = 0, mine = 0;
-  if (tid < p.E)
-    for (int b = 0; b < p.blocks; ++b) {
-      const int* f = p.block_first + (size_t)b * (p.E + 1) + tid;
-      const int lo = __ldcg(f), n = __ldcg(f + 1) - lo;
-      if (b < me) before += n;
-      if (b == me) mine = lo;
-      count += n;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int base = blockIdx.x * p.chunk, me = base / kMpSortPairs;
+  int rows = 0, tiles = 0, padded = 0;
+  for (int e0 = 0; e0 < p.E; e0 += kMpPlaceThreads) {
+    const int e = e0 + tid;
+    int count = 0, before = 0;
+    if (e < p.E) {
+      if (p.ids) {
+#pragma unroll 4
+        for (int b = 0; b < p.blocks; ++b) {
+          const int n = __ldcg(p.hist + (size_t)b * p.E + e);
+          count += n;
+          before += b < me ? n : 0;
+        }
+      } else {
+        count = p.pairs;
+      }
     }
-  int total;
-  const int first = mp_scan<kMpSortThreads>(count, s_sums, &total);
-  if (me == 0 && tid <= p.E) p.first[tid] = first;
-  if (me == 0 && p.E == kMpSortThreads && tid == 0) p.first[p.E] = total;
-  s_at[tid] = first + before - mine;  // what to add to a place in the block's list
+    const MpTiles t = mp_tiles(count, p.tile);
+    int total;
+    const int f = rows + mp_scan<kMpPlaceThreads>(count, s_sums, &total);
+    rows += total;
+    const int o = tiles + mp_scan<kMpPlaceThreads>(t.n, s_sums, &total);
+    tiles += total;
+    const int r = padded + mp_scan<kMpPlaceThreads>(t.n * t.each, s_sums, &total);
+    padded += total;
+    if (e < p.E) {
+      s_first[e] = f, s_before[e] = before, s_count[e] = count, s_tile[e] = o, s_row[e] = r;
+      if (blockIdx.x == 0) p.first[e] = f;
+    }
+  }
+  if (blockIdx.x == 0 && tid == 0) p.first[p.E] = rows;
   __syncthreads();
-  const int* src = p.block_list + (size_t)me * kMpSortPairs;
-  const int n = __ldcg(p.block_first + (size_t)me * (p.E + 1) + p.E);
-  for (int i = tid; i < n; i += kMpSortThreads) {
-    int lo = 0, hi = p.E - 1;  // the last expert whose first place is not above i
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (__ldcg(p.block_first + (size_t)me * (p.E + 1) + mid) <= i) lo = mid; else hi = mid - 1;
+  const int chunks = mx_chunks(p.K), atoms = mx_atoms(p.K), pieces = 2 * chunks, kbytes = p.K >> 1, halves = (p.tile + 127) >> 7;
+  for (int i = warp * 8; i < p.chunk; i += kMpPlaceThreads / 32 * 8) {
+    const int pair = base + i + (lane & 7);
+    int e = -1, pos = 0;
+    if (pair < p.pairs) {
+      e = p.ids ? __ldcg(p.ids + pair) : 0;
+      if ((unsigned)e >= (unsigned)p.E) e = -1;
+      else pos = p.ids ? s_before[e] + __ldcg(p.rank + pair) : pair;
     }
-    p.list[s_at[lo] + i] = __ldcg(src + i);
+    if (e < 0) continue;  // no lane waits for another
+    const MpTiles t = mp_tiles(s_count[e], p.tile);
+    const int tile = pos / t.each, r = pos - tile * t.each;
+    const int64_t x = p.x_per_pair ? pair : pair / p.k;
+    const uint8_t* src = p.codes + x * kbytes;
+    uint8_t* dst = p.t_codes + (size_t)(s_row[e] + tile * t.each) * chunks * (kMxChunk / 2) + r * 16;
+#pragma unroll 8
+    for (int q = lane >> 3; q < pieces; q += 4) {
+      const uint4 v = q * 16 < kbytes ? __ldcg(reinterpret_cast<const uint4*>(src) + q) : make_uint4(0, 0, 0, 0);
+      *reinterpret_cast<uint4*>(dst + (size_t)q * t.each * 16) = v;
+    }
+    const uint32_t* s = reinterpret_cast<const uint32_t*>(p.scale + x * (4 * atoms));
+    uint8_t* sd = p.t_scale + (size_t)(s_tile[e] + tile) * atoms * halves * kMxAtomBytes + (r >> 7) * kMxAtomBytes + (r & 31) * 16 + ((r >> 5) & 3) * 4;
+#pragma unroll 4
+    for (int j = lane >> 3; j < atoms; j += 4) {
+      const int left = (p.K >> 5) - 4 * j;
+      uint32_t w = __ldcg(s + j);
+      if (left < 4) w &= (1u << (8 * left)) - 1u;  // bytes beyond the row's end
+      *reinterpret_cast<uint32_t*>(sd + (size_t)j * halves * kMxAtomBytes) = w;
+    }
+    if (lane < 8) p.list[s_first[e] + pos] = pair;
   }
 }
 
 // ---- the product ----------------------------------------------------------------------------------------------------
-constexpr int kMpTile = 224;                 // most tokens of a tile
 constexpr int kMpStepChunks = 4;             // chunks of 64 values a step
-constexpr int kMpGatherWarps = 6, kMpDrainWarps = 8;
-constexpr int kMpWeightWarp = 0, kMpMmaWarp = 1, kMpFirstGather = 2, kMpFirstDrain = 8;
-constexpr int kMpThreads = 32 * (kMpFirstDrain + kMpDrainWarps);
-constexpr int kMpPlanWarp = kMpFirstDrain + kMpDrainWarps;  // one more warp
-constexpr int kMpAllThreads = kMpThreads + 32;
+// Warps: weights (and tiles), products, plan; then, from the fourth on, eight that drain; the rows' gatherers are the third and those behind.
+constexpr int kMpWeightWarp = 0, kMpMmaWarp = 1, kMpPlanWarp = 2, kMpFirstDrain = 4, kMpDrainWarps = 8, kMpGatherWarps = 6;
+constexpr int kMpTable = 128;                // table entries that a CTA keeps in shared memory
+__host__ __device__ constexpr int mp_threads(bool placed) { return 32 * (kMpFirstDrain + kMpDrainWarps + (placed ? 0 : kMpGatherWarps - 1)); }
 constexpr int kMpSlots = 4, kMpMaxStages = 8;
 constexpr int kMpTmemCols = 512;
 constexpr int kMpScaleCol = 2 * kMpTile;     // behind the two accumulators: scales of two steps, 8 + 16 columns each
@@ -160,10 +211,12 @@ static_assert(kMpScaleCol + 2 * kMpScaleCols <= kMpTmemCols, "tensor memory");
 constexpr int kMpABytes = kMpStepChunks * kMxChunkBytes, kMpAScaleBytes = kMpStepChunks / 2 * kMxAtomBytes;
 
 struct MpItem {
-  const uint8_t *codes, *scale;
+  const uint8_t *codes, *scale;      // the row block's weights
+  const uint8_t *t_codes, *t_scale;  // the placed tile
   int n;         // tokens; < 0: no more items
+  int rows;      // rows of the tile as it lies, a multiple of 16
   int rb;        // row block
-  int pad_[2];
+  int pad_;
 };
 struct __align__(16) MpSmem {
   unsigned long long full_a[kMpMaxStages], full_b[kMpMaxStages], free_[kMpMaxStages];
@@ -174,8 +227,10 @@ struct __align__(16) MpSmem {
   unsigned long long limit;  // 8 bytes behind dead
   MpItem item[kMpSlots];
   int pair[kMpSlots][kMpTile], row[kMpSlots][kMpTile];
+  slicemoe_mx4_mat mats[kMpTable];
   int first[kMpMaxExperts + 1];  // rows before an expert
-  int items[kMpMaxExperts + 1];  // items before it
+  int tiles[kMpMaxExperts + 1];  // tiles before it
+  int padded[kMpMaxExperts];     // rows of the tiles before it
   int list[kMpInline];
   int sums[32];
 };
@@ -190,7 +245,8 @@ struct MpParams {
   const int32_t* ids;
   void* out;
   MpHeader* head;
-  const int *first, *list;
+  const int *first, *list;             // of the placed rows
+  const uint8_t *t_codes, *t_scale;
   int E, N, K, gated, T, k, x_per_pair;
   int tile, stages;      // most tokens of a tile here, a multiple of 16; steps of the ring
   int row_blocks;
@@ -254,8 +310,9 @@ __device__ __forceinline__ uint32_t mp_pack2(float a, float b) {
   return w;
 }
 
-template <class O, bool GATED>
-__global__ void __launch_bounds__(kMpAllThreads, 1) mp_product_kernel(const MpParams p) {
+template <class O, bool GATED, bool PLACED>
+__global__ void __launch_bounds__(mp_threads(PLACED), 1) mp_product_kernel(const MpParams p) {
+  constexpr int kThreads = mp_threads(PLACED);
   extern __shared__ __align__(128) uint8_t mp_smem[];
   MpSmem* s = reinterpret_cast<MpSmem*>(mp_smem);
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
@@ -278,7 +335,7 @@ __global__ void __launch_bounds__(kMpAllThreads, 1) mp_product_kernel(const MpPa
     }
     for (int i = 0; i < kMpSlots; ++i) {
       mbar_init(smem_u32(&s->item_full[i]), 1);
-      mbar_init(smem_u32(&s->item_free[i]), 2 + kMpGatherWarps + kMpDrainWarps);
+      mbar_init(smem_u32(&s->item_free[i]), 2 + (PLACED ? 0 : kMpGatherWarps) + kMpDrainWarps);
     }
     mbar_init(smem_u32(&s->drain), 1);
     s->dead = 0;
@@ -289,82 +346,62 @@ __global__ void __launch_bounds__(kMpAllThreads, 1) mp_product_kernel(const MpPa
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   // the table does not change between launches: it is read while the kernel before is still at work
-  bool fits[(kMpMaxExperts + kMpAllThreads - 1) / kMpAllThreads];
-  constexpr int kEach = sizeof(fits) / sizeof(fits[0]);
-#pragma unroll
-  for (int i = 0; i < kEach; ++i) {
-    const int e = i * kMpAllThreads + tid;
-    fits[i] = false;
-    if (e < p.E) {
-      const slicemoe_mx4_mat m = p.mats[e];
-      fits[i] = m.codes && m.scale && m.N == p.N && m.K == p.K && (m.gated != 0) == GATED;
-      s->first[e] = 0;
-    }
+  if (p.E <= kMpTable) {
+    constexpr int kWords = sizeof(slicemoe_mx4_mat) / 8;
+    for (int i = tid; i < p.E * kWords; i += kThreads)
+      reinterpret_cast<unsigned long long*>(s->mats)[i] = __ldg(reinterpret_cast<const unsigned long long*>(p.mats) + i);
   }
+  for (int e = tid; e <= p.E; e += kThreads) s->first[e] = 0;
   mx_dep_wait();
   if (tid == 0) s->limit = p.head->wait_cycles ? p.head->wait_cycles : kWaitCycles;
-  const bool own_list = p.ids && !p.list;
-  int total_rows = p.T;
-  if (own_list) {  // few pairs: by expert, here
+  int rank = 0, e_mine = -1;
+  if constexpr (PLACED) {
+    for (int e = tid; e <= p.E; e += kThreads) s->first[e] = __ldcg(p.first + e);
+  } else if (p.ids) {  // few pairs: by expert, here
     const int pairs = p.T * p.k;
     __syncthreads();
-    const int e = tid < pairs ? __ldcg(p.ids + tid) : -1;
-    const bool named = (unsigned)e < (unsigned)p.E;
+    e_mine = tid < pairs ? __ldcg(p.ids + tid) : -1;
+    if ((unsigned)e_mine >= (unsigned)p.E) e_mine = -1;
+    if (tid < pairs && e_mine < 0 && blockIdx.x == 0) atomicOr(status, (unsigned)SLICEMOE_STATUS_BAD_EXPERT_ID);
     // in the order of the list, warp after warp: all CTAs must deal the same pairs to the same tiles
-    int rank = 0;
-    const unsigned same = __match_any_sync(0xffffffffu, e), lower = same & ((1u << lane) - 1u);
+    const unsigned same = __match_any_sync(0xffffffffu, e_mine), lower = same & ((1u << lane) - 1u);
     for (int w = 0; w * 32 < pairs; ++w) {
-      if (warp == w && named) rank = s->first[e] + __popc(lower);
+      if (warp == w && e_mine >= 0) rank = s->first[e_mine] + __popc(lower);
       __syncwarp();
-      if (warp == w && named && lower == 0) s->first[e] += __popc(same);
+      if (warp == w && e_mine >= 0 && lower == 0) s->first[e_mine] += __popc(same);
       __syncthreads();
     }
-    if (tid < pairs && !named && blockIdx.x == 0) atomicOr(status, (unsigned)SLICEMOE_STATUS_BAD_EXPERT_ID);
-    int count[kEach], before[kEach], base = 0;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const int x = i * kMpAllThreads + tid;
-      count[i] = x < p.E ? s->first[x] : 0;
-      before[i] = 0;
-      if (i * kMpAllThreads < p.E) {
-        int total;
-        before[i] = base + mp_scan<kMpAllThreads>(count[i], s->sums, &total);
-        base += total;
-      }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const int x = i * kMpAllThreads + tid;
-      if (x < p.E) s->first[x] = before[i];
-    }
-    total_rows = base;
-    __syncthreads();
-    if (named) s->list[s->first[e] + rank] = tid;
-  } else if (p.list) {
-    for (int i = tid; i < p.E; i += kMpAllThreads) s->first[i] = __ldcg(p.first + i);
-    total_rows = __ldcg(p.first + p.E);
   } else {
-    for (int i = tid; i < p.E; i += kMpAllThreads) s->first[i] = i ? p.T : 0;
+    for (int e = tid; e <= p.E; e += kThreads) s->first[e] = e ? p.T : 0;
   }
-  if (tid == 0) s->first[p.E] = total_rows;
   __syncthreads();
-  int total_items = 0;
-#pragma unroll
-  for (int i = 0; i < kEach; ++i) {
-    const int e = i * kMpAllThreads + tid;
-    if (i * kMpAllThreads >= p.E) break;
-    int n = e < p.E ? s->first[e + 1] - s->first[e] : 0;
-    if (n > 0 && !fits[i]) {
-      n = 0;
-      if (blockIdx.x == 0) atomicOr(status, (unsigned)SLICEMOE_STATUS_BAD_EXPERT_ID);
+  int tiles = 0, rows = 0, padded = 0;
+  for (int e0 = 0; e0 < p.E; e0 += kThreads) {
+    const int e = e0 + tid;
+    int count = 0, total;
+    if (e < p.E) count = !PLACED && p.ids ? s->first[e] : s->first[e + 1] - s->first[e];
+    const MpTiles t = mp_tiles(count, p.tile);
+    const int o = tiles + mp_scan<kThreads>(t.n, s->sums, &total);
+    tiles += total;
+    if (e < p.E) s->tiles[e] = o;
+    if constexpr (PLACED) {
+      const int r = padded + mp_scan<kThreads>(t.n * t.each, s->sums, &total);
+      padded += total;
+      if (e < p.E) s->padded[e] = r;
+    } else if (p.ids) {
+      const int f = rows + mp_scan<kThreads>(count, s->sums, &total);  // its barriers lie between the reads of first[] and this write
+      rows += total;
+      if (e < p.E) s->first[e] = f;
     }
-    int total;
-    const int before = mp_scan<kMpAllThreads>((n + p.tile - 1) / p.tile * p.row_blocks, s->sums, &total);
-    if (e < p.E) s->items[e] = total_items + before;
-    total_items += total;
   }
-  if (tid == 0) s->items[p.E] = total_items;
+  if constexpr (!PLACED) {
+    if (p.ids) {
+      if (tid == 0) s->first[p.E] = rows;
+      __syncthreads();
+      if (e_mine >= 0) s->list[s->first[e_mine] + rank] = tid;
+    }
+  }
+  const int total_items = tiles * p.row_blocks;
   mp_fence_before();
   __syncthreads();
   mp_fence_after();
@@ -383,26 +420,40 @@ __global__ void __launch_bounds__(kMpAllThreads, 1) mp_product_kernel(const MpPa
         if (lane == 0) mbar_arrive(smem_u32(&s->item_full[slot]));
         break;
       }
-      int lo = 0;  // the last expert whose first item is not above `it`; two steps of 32 lanes
-      const int cut = lane * 32;
-      lo = 32 * (__popc(__ballot_sync(0xffffffffu, cut < p.E && s->items[cut] <= it)) - 1);
-      lo += __popc(__ballot_sync(0xffffffffu, lo + lane < p.E && s->items[lo + lane] <= it)) - 1;
-      const slicemoe_mx4_mat* m = p.mats + lo;
-      const uint8_t *codes = m->codes, *scale = m->scale;
-      const int first = s->first[lo], count = s->first[lo + 1] - first, local = it - s->items[lo];
-      const int tiles = (count + p.tile - 1) / p.tile, rb = local / tiles, t = local - rb * tiles;
-      const int each = ((count + tiles - 1) / tiles + 15) & ~15, r0 = t * each, n = min(each, count - r0);
+      // its expert: the last one whose first tile is not above the item's (in tiles of all row blocks); two steps of 32 lanes
+      const int at = it / p.row_blocks;
+      int e = 32 * (__popc(__ballot_sync(0xffffffffu, lane * 32 < p.E && s->tiles[lane * 32] <= at)) - 1);
+      e += __popc(__ballot_sync(0xffffffffu, e + lane < p.E && s->tiles[e + lane] <= at)) - 1;
+      const slicemoe_mx4_mat m = p.E <= kMpTable ? s->mats[e] : p.mats[e];
+      if (!m.codes || !m.scale || m.N != p.N || m.K != p.K || (m.gated != 0) != GATED) {
+        if (lane == 0) atomicOr(status, (unsigned)SLICEMOE_STATUS_BAD_EXPERT_ID);
+        continue;
+      }
+      // of an expert's items a row block's tiles come one after the other: its weights are in L2 for all but the first
+      const int first = s->first[e], count = s->first[e + 1] - first, local = it - s->tiles[e] * p.row_blocks;
+      const MpTiles tt = mp_tiles(count, p.tile);
+      const int rb = local / tt.n, t = local - rb * tt.n, r0 = t * tt.each, n = min(tt.each, count - r0);
       for (int i = lane; i < n; i += 32) {
         const int at = first + r0 + i;
-        const int pair = own_list ? s->list[at] : p.list ? __ldcg(p.list + at) : at;
-        s->pair[slot][i] = pair;
-        s->row[slot][i] = p.x_per_pair ? pair : pair / p.k;
+        if constexpr (PLACED) {
+          s->pair[slot][i] = __ldcg(p.list + at);
+        } else {
+          const int pair = p.ids ? s->list[at] : at;
+          s->pair[slot][i] = pair;
+          s->row[slot][i] = p.x_per_pair ? pair : pair / p.k;
+        }
       }
       if (lane == 0) {
-        s->item[slot].codes = codes + (size_t)rb * chunks * kMxChunkBytes;
-        s->item[slot].scale = scale + (size_t)rb * atoms * kMxAtomBytes;
-        s->item[slot].n = n;
-        s->item[slot].rb = rb;
+        MpItem* item = &s->item[slot];
+        item->codes = m.codes + (size_t)rb * chunks * kMxChunkBytes;
+        item->scale = m.scale + (size_t)rb * atoms * kMxAtomBytes;
+        item->n = n;
+        item->rows = PLACED ? tt.each : p.tile;
+        item->rb = rb;
+        if constexpr (PLACED) {
+          item->t_codes = p.t_codes + (size_t)(s->padded[e] + r0) * chunks * (kMxChunk / 2);
+          item->t_scale = p.t_scale + (size_t)(s->tiles[e] + t) * atoms * halves * kMxAtomBytes;
+        }
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&s->item_full[slot]));
@@ -412,6 +463,7 @@ __global__ void __launch_bounds__(kMpAllThreads, 1) mp_product_kernel(const MpPa
     // ---- weights ----
     uint32_t slot = 0, turn = 0, st = 0, ph = 0, filled = 0;
     const bool bring = p.head->extra_arrivals == 0;
+    if constexpr (PLACED) asm volatile("fence.proxy.async;" ::: "memory");  // the tiles were written by ordinary stores
     bool ok = true;
     while (ok && (ok = mp_wait(&s->item_full[slot], turn, s, status))) {
       const MpItem item = s->item[slot];
@@ -421,9 +473,14 @@ __global__ void __launch_bounds__(kMpAllThreads, 1) mp_product_kernel(const MpPa
         const int c = min(kMpStepChunks, chunks - i * kMpStepChunks), a = (c + 1) >> 1;
         if (bring && mp_elect()) {
           const uint32_t dst = ring + st * stage_bytes, bar = smem_u32(&s->full_a[st]);
-          mbar_arrive_expect_tx(bar, c * kMxChunkBytes + a * kMxAtomBytes);
+          const uint32_t t_bytes = PLACED ? c * item.rows * (kMxChunk / 2) : 0, ts_bytes = PLACED ? a * halves * kMxAtomBytes : 0;
+          mbar_arrive_expect_tx(bar, c * kMxChunkBytes + a * kMxAtomBytes + t_bytes + ts_bytes);
           mp_bulk(dst, item.codes + (size_t)i * kMpABytes, c * kMxChunkBytes, bar);
           mp_bulk(dst + kMpABytes, item.scale + (size_t)i * kMpAScaleBytes, a * kMxAtomBytes, bar);
+          if constexpr (PLACED) {
+            mp_bulk(dst + kMpABytes + kMpAScaleBytes, item.t_codes + (size_t)i * item.rows * (kMpStepChunks * kMxChunk / 2), t_bytes, bar);
+            mp_bulk(dst + kMpABytes + kMpAScaleBytes + b_bytes, item.t_scale + (size_t)i * halves * kMpAScaleBytes, ts_bytes, bar);
+          }
         }
         __syncwarp();
         ++filled;
@@ -447,7 +504,7 @@ __global__ void __launch_bounds__(kMpAllThreads, 1) mp_product_kernel(const MpPa
     uint32_t slot = 0, turn = 0, st = 0, ph = 0, acc = 0, acc_ph = 0, flip = 0;
     bool ok = true;
     while (ok && (ok = mp_wait(&s->item_full[slot], turn, s, status))) {
-      const int n = s->item[slot].n;
+      const int n = s->item[slot].n, rows = s->item[slot].rows;
       if (n < 0) break;
       const uint32_t idesc = mp_idesc((n + 15) & ~15), d = tmem + acc * kMpTile;
       const int blocks = (n + 127) >> 7;
@@ -455,7 +512,7 @@ __global__ void __launch_bounds__(kMpAllThreads, 1) mp_product_kernel(const MpPa
       mp_fence_after();
       for (int i = 0; i < steps; ++i) {
         if (!(ok = mp_wait(&s->full_a[st], ph, s, status))) break;
-        if (!(ok = mp_wait(&s->full_b[st], ph, s, status))) break;
+        if (!PLACED && !(ok = mp_wait(&s->full_b[st], ph, s, status))) break;
         mp_fence_after();
         const int c = min(kMpStepChunks, chunks - i * kMpStepChunks), a = (c + 1) >> 1;
         if (mp_elect()) {
@@ -467,7 +524,7 @@ __global__ void __launch_bounds__(kMpAllThreads, 1) mp_product_kernel(const MpPa
           }
           for (int j = 0; j < c; ++j) {
             const uint32_t half = (uint32_t)(j & 1) * 2u;
-            mp_mma(d, mp_desc(at + j * kMxChunkBytes, kMxRows * 16, 128), mp_desc(b_at + j * p.tile * 32, p.tile * 16, 128),
+            mp_mma(d, mp_desc(at + j * kMxChunkBytes, kMxRows * 16, 128), mp_desc(b_at + j * rows * 32, rows * 16, 128),
                    idesc | half << 29 | half << 4, sa + 4 * (j >> 1), sb + 8 * (j >> 1), (i | j) != 0);
           }
           mp_commit(smem_u32(&s->free_[st]));
@@ -488,9 +545,10 @@ __global__ void __launch_bounds__(kMpAllThreads, 1) mp_product_kernel(const MpPa
     const long long t0 = clock64();
     while (!mbar_try(smem_u32(&s->drain), 0) && clock64() - t0 < 4000000ll) {
     }
-  } else if (warp < kMpFirstDrain) {
-    // ---- token rows: the warps bring the steps in turn ----
-    const int me = warp - kMpFirstGather;
+  } else if (warp < kMpFirstDrain || warp >= kMpFirstDrain + kMpDrainWarps) {
+    // ---- token rows, where they are not placed: the warps bring the steps in turn ----
+    if constexpr (!PLACED) {
+    const int me = warp < kMpFirstDrain ? 0 : warp - (kMpFirstDrain + kMpDrainWarps) + 1;
     uint32_t slot = 0, turn = 0, st = 0, ph = 0;
     // No more warps take turns than the ring has steps.  A warp's next step is then at most one round of the ring ahead of one that
     // it has waited for, and the parity of a barrier tells it what it needs: with more it could be two rounds ahead.
@@ -507,17 +565,19 @@ __global__ void __launch_bounds__(kMpAllThreads, 1) mp_product_kernel(const MpPa
           if (!(ok = mp_wait(&s->free_[st], ph ^ 1u, s, status))) break;
           const int c = min(kMpStepChunks, chunks - i * kMpStepChunks), a = (c + 1) >> 1;
           const uint32_t dst = ring + st * stage_bytes + kMpABytes + kMpAScaleBytes, sdst = dst + b_bytes;
-          // scales: a word of four per row and 128 values, bytes beyond the row's end cleared
-          for (int r = lane; r < n; r += 32) {
-            const uint8_t* src = p.scale + (size_t)rows[r] * pitch + i * (2 * kMpStepChunks);
-            for (int j = 0; j < a; ++j) {
-              uint32_t w = __ldcg(reinterpret_cast<const uint32_t*>(src) + j);
-              const int left = (p.K >> 5) - (i * (kMpStepChunks / 2) + j) * 4;
-              if (left < 4) w &= (1u << (8 * left)) - 1u;
-              asm volatile("st.shared.b32 [%0], %1;" ::"r"(sdst + (j * halves + (r >> 7)) * kMxAtomBytes + (r & 31) * 16 + ((r >> 5) & 3) * 4), "r"(w) : "memory");
-            }
+          // scales: a word of four per row and 128 values, bytes beyond the row's end cleared.  All of a lane's loads are under way
+          // before the first is used (one after the other they took longer than everything else: 16 us an item, not 2)
+          constexpr int kRows = kMpTile / 32, kWords = kMpStepChunks / 2;
+          uint32_t w[kRows][kWords];
+#pragma unroll
+          for (int q = 0; q < kRows; ++q) {
+            const int r = q * 32 + lane;
+            const uint8_t* src = p.scale + (size_t)(r < n ? rows[r] : 0) * pitch + i * (2 * kMpStepChunks);
+#pragma unroll
+            for (int j = 0; j < kWords; ++j) w[q][j] = r < n && j < a ? __ldcg(reinterpret_cast<const uint32_t*>(src) + j) : 0u;
           }
           // codes: eight rows x four pieces of 16 bytes a step of the warp; a shared-memory write is eight rows side by side
+#pragma unroll 4
           for (int r = lane & 7; r < n; r += 8) {
             const uint8_t* src = p.codes + (size_t)rows[r] * kbytes;
 #pragma unroll
@@ -527,6 +587,18 @@ __global__ void __launch_bounds__(kMpAllThreads, 1) mp_product_kernel(const MpPa
                 const bool in = at < kbytes;
                 mp_cp16(dst + (piece >> 1) * p.tile * 32 + (piece & 1) * p.tile * 16 + r * 16, in ? src + at : src, in ? 16u : 0u);
               }
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < kWords; ++j) {
+            const int left = (p.K >> 5) - (i * kWords + j) * 4;
+            const uint32_t mask = left < 4 ? (1u << (8 * max(left, 0))) - 1u : 0xffffffffu;
+#pragma unroll
+            for (int q = 0; q < kRows; ++q) {
+              const int r = q * 32 + lane;
+              if (r < n && j < a)
+                asm volatile("st.shared.b32 [%0], %1;" ::"r"(sdst + (j * halves + (q >> 2)) * kMxAtomBytes + lane * 16 + (q & 3) * 4), "r"(w[q][j] & mask)
+                             : "memory");
             }
           }
           asm volatile("cp.async.wait_all;" ::: "memory");
@@ -540,6 +612,7 @@ __global__ void __launch_bounds__(kMpAllThreads, 1) mp_product_kernel(const MpPa
       if (!ok) break;
       if (lane == 0) mbar_arrive(smem_u32(&s->item_free[slot]));
       if (++slot == kMpSlots) slot = 0, turn ^= 1u;
+    }
     }
   } else {
     // ---- results: a warp reads 32 weight rows, 16 tokens at a time, every other sixteen ----
@@ -608,7 +681,10 @@ __global__ void __launch_bounds__(kMpAllThreads, 1) mp_product_kernel(const MpPa
   if (warp == kMpMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kMpTmemCols) : "memory");
 }
 
-template <class O, bool GATED>
+static int mp_stage_bytes(int tile) {
+  return kMpABytes + kMpAScaleBytes + tile * (kMpStepChunks * kMxChunk / 2) + (tile + 127) / 128 * kMpAScaleBytes;
+}
+template <class O, bool GATED, bool PLACED>
 static int mp_launch(const MpParams& p, int items, cudaStream_t st) {
   static bool attr_set[64];
   static int sm_count[64];
@@ -616,27 +692,28 @@ static int mp_launch(const MpParams& p, int items, cudaStream_t st) {
   SM_CUDA_TRY(cudaGetDevice(&dev));
   if (dev < 0 || dev >= 64) return SLICEMOE_E_UNSUPPORTED;
   if (!attr_set[dev]) {
-    SM_CUDA_TRY(cudaFuncSetAttribute(mp_product_kernel<O, GATED>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMpSmemMax));
+    SM_CUDA_TRY(cudaFuncSetAttribute(mp_product_kernel<O, GATED, PLACED>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMpSmemMax));
     SM_CUDA_TRY(cudaDeviceGetAttribute(&sm_count[dev], cudaDevAttrMultiProcessorCount, dev));
     attr_set[dev] = true;
   }
-  const int stage = kMpABytes + kMpAScaleBytes + p.tile * (kMpStepChunks * kMxChunk / 2) + (p.tile + 127) / 128 * kMpAScaleBytes;
-  const int smem = kMpFixed + p.stages * stage;
-  return mx_launch(mp_product_kernel<O, GATED>, dim3(items < sm_count[dev] ? items : sm_count[dev]), kMpAllThreads,
+  const int smem = kMpFixed + p.stages * mp_stage_bytes(p.tile);
+  return mx_launch(mp_product_kernel<O, GATED, PLACED>, dim3(items < sm_count[dev] ? items : sm_count[dev]), mp_threads(PLACED),
                    (size_t)(smem > kMpSmemMin ? smem : kMpSmemMin), st, MpParams(p));
 }
 template <class O>
 static int mp_launch_as(const MpParams& p, int items, cudaStream_t st) {
-  return p.gated ? mp_launch<O, true>(p, items, st) : mp_launch<O, false>(p, items, st);
+  if (p.t_codes) return p.gated ? mp_launch<O, true, true>(p, items, st) : mp_launch<O, false, true>(p, items, st);
+  return p.gated ? mp_launch<O, true, false>(p, items, st) : mp_launch<O, false, false>(p, items, st);
 }
 
 }  // namespace slicemoe
 
 using namespace slicemoe;
 
-extern "C" size_t slicemoe_mx4_workspace_bytes(int T, int k, int n_experts) {
+extern "C" size_t slicemoe_mx4_workspace_bytes(int T, int k, int n_experts, int K) {
   if (T <= 0 || k < 1 || k > SLICEMOE_MAX_TOP_K || n_experts <= 0 || n_experts > kMpMaxExperts || (int64_t)T * k > kMpMaxPairs) return 0;
-  return mp_layout((int64_t)T * k, n_experts).total;
+  if (K <= 0 || K % kMxBlock || K > kMxMaxK) return 0;
+  return mp_layout(T, k, n_experts, K).total;
 }
 
 extern "C" int slicemoe_mx4_workspace_init(void* workspace, size_t workspace_bytes, void* stream) {
@@ -652,8 +729,8 @@ extern "C" int slicemoe_mx4_product(const slicemoe_mx4_mat* mats, int n_experts,
   if (n_experts <= 0 || N <= 0 || K <= 0 || K % kMxBlock || T <= 0 || k < 1 || (!ids && k != 1)) return SLICEMOE_E_INVALID_ARG;
   if (n_experts > kMpMaxExperts || N > kMxMaxN || K > kMxMaxK || k > SLICEMOE_MAX_TOP_K || (int64_t)T * k > kMpMaxPairs || !mx_dtype(dtype))
     return SLICEMOE_E_UNSUPPORTED;
-  const int pairs = T * k;
-  const MpLayout l = mp_layout(pairs, n_experts);
+  const int pairs = T * k, E = ids ? n_experts : 1;
+  const MpLayout l = mp_layout(T, k, E, K);
   if (!mx_aligned(mats, 8) || !mx_aligned(codes, 16) || !mx_aligned(scale, 4) || !mx_aligned(out, 16) || !mx_aligned(ids, 4) ||
       !mx_aligned(workspace, 256) || workspace_bytes < l.total)
     return SLICEMOE_E_INVALID_ARG;
@@ -666,34 +743,35 @@ extern "C" int slicemoe_mx4_product(const slicemoe_mx4_mat* mats, int n_experts,
   p.ids = ids;
   p.out = out;
   p.head = reinterpret_cast<MpHeader*>(ws);
-  p.E = ids ? n_experts : 1;
+  p.E = E;
   p.N = N;
   p.K = K;
   p.gated = gated;
   p.T = T;
   p.k = k;
   p.x_per_pair = x_per_pair;
-  // an expert has at most T rows where no token names one twice: wider tiles would only take room from the ring
-  p.tile = T >= kMpTile ? kMpTile : (T + 15) & ~15;
-  const int stage = kMpABytes + kMpAScaleBytes + p.tile * (kMpStepChunks * kMxChunk / 2) + (p.tile + 127) / 128 * kMpAScaleBytes;
-  p.stages = (kMpSmemMax - kMpFixed) / stage;
+  p.tile = mp_tile(T);
+  p.stages = (kMpSmemMax - kMpFixed) / mp_stage_bytes(p.tile);
   if (p.stages > kMpMaxStages) p.stages = kMpMaxStages;
   p.row_blocks = mx_row_blocks(N, gated);
-  const int64_t tiles = (int64_t)pairs / p.tile + (pairs < p.E ? pairs : p.E), items = tiles * p.row_blocks;
+  const int64_t tiles = (int64_t)pairs / p.tile + (pairs < E ? pairs : E), items = tiles * p.row_blocks;
   if (items > INT32_MAX) return SLICEMOE_E_UNSUPPORTED;
-  if (ids && pairs > kMpInline) {
-    int* first = reinterpret_cast<int*>(ws + l.first);
-    int* list = reinterpret_cast<int*>(ws + l.list);
-    int* block_first = l.blocks > 1 ? reinterpret_cast<int*>(ws + l.block_first) : first;
-    int* block_list = l.blocks > 1 ? reinterpret_cast<int*>(ws + l.block_list) : list;
-    int rc = mx_launch(mp_sort_kernel, dim3(l.blocks), kMpSortThreads, 0, st, MpSortParams{ids, pairs, n_experts, block_first, block_list, p.head});
-    if (rc != SLICEMOE_OK) return rc;
-    if (l.blocks > 1) {
-      rc = mx_launch(mp_merge_kernel, dim3(l.blocks), kMpSortThreads, 0, st, MpMergeParams{block_first, block_list, l.blocks, n_experts, first, list});
+  if (pairs > kMpInline) {
+    int *rank = reinterpret_cast<int*>(ws + l.rank), *hist = reinterpret_cast<int*>(ws + l.hist), *first = reinterpret_cast<int*>(ws + l.first),
+        *list = reinterpret_cast<int*>(ws + l.list);
+    if (ids) {
+      const int rc = mx_launch(mp_sort_kernel, dim3(l.blocks), kMpSortThreads, 0, st, MpSortParams{ids, pairs, E, rank, hist, p.head});
       if (rc != SLICEMOE_OK) return rc;
     }
+    int chunk = 64;  // pairs of a block: more where there are blocks enough to fill the device
+    while (chunk < kMpSortPairs && pairs / chunk > 1184) chunk *= 2;
+    const MpPlaceParams pp = {ids, rank, hist, codes, scale, first, list, ws + l.codes, ws + l.scale, pairs, E, l.blocks, chunk, p.tile, k, x_per_pair, K};
+    const int rc = mx_launch(mp_place_kernel, dim3((pairs + chunk - 1) / chunk), kMpPlaceThreads, 0, st, MpPlaceParams(pp));
+    if (rc != SLICEMOE_OK) return rc;
     p.first = first;
     p.list = list;
+    p.t_codes = ws + l.codes;
+    p.t_scale = ws + l.scale;
   }
   if (dtype == SLICEMOE_F32) return mp_launch_as<float>(p, (int)items, st);
   if (dtype == SLICEMOE_BF16) return mp_launch_as<__nv_bfloat16>(p, (int)items, st);

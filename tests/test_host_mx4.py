@@ -50,9 +50,13 @@ def test_sizes():
     assert L.slicemoe_mx4_codes_bytes(64, 64, 1) == 4096 and L.slicemoe_mx4_codes_bytes(65, 64, 1) == 2 * 4096
     assert L.slicemoe_mx4_scale_bytes(128, 64, 0) == 512 and L.slicemoe_mx4_scale_bytes(1408, 2048, 1) == 22 * 16 * 512
     assert L.slicemoe_mx4_codes_bytes(0, 64, 0) == 0 and L.slicemoe_mx4_codes_bytes(16, 48, 0) == 0
-    assert L.slicemoe_mx4_workspace_bytes(0, 1, 1) == 0 and L.slicemoe_mx4_workspace_bytes(1, 17, 1) == 0
-    assert L.slicemoe_mx4_workspace_bytes(1, 1, 1025) == 0 and L.slicemoe_mx4_workspace_bytes(1 << 21, 16, 8) == 0
-    assert L.slicemoe_mx4_workspace_bytes(1, 6, 64) >= 256
+    ws = L.slicemoe_mx4_workspace_bytes
+    assert ws(0, 1, 1, 64) == 0 and ws(1, 17, 1, 64) == 0 and ws(1, 1, 1025, 64) == 0 and ws(1 << 21, 16, 8, 64) == 0 and ws(1, 1, 1, 48) == 0
+    assert ws(1, 6, 64, 2048) >= 256
+    for T in (1, 5, 16, 100, 223, 224, 225, 1000, 5000):          # one of a larger call serves smaller ones
+        for k in (1, 3, 16):
+            for E in (1, 8, 1000):
+                assert all(ws(T, k, E, 160) <= ws(*more) for more in ((T + 1, k, E, 160), (T, min(k + 1, 16), E, 160), (T, k, E + 1, 160), (T, k, E, 192)))
 
 
 @pytest.mark.parametrize("kw,rc", [(dict(W=None), -1), (dict(N=0), -1), (dict(K=33), -1), (dict(ld=10), -1), (dict(W=p(4098)), -1), (dict(up=p(4098)), -1),
