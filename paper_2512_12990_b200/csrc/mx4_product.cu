@@ -203,7 +203,7 @@ constexpr int kMpStepChunks = 4;             // chunks of 64 values a step
 constexpr int kMpWeightWarp = 0, kMpMmaWarp = 1, kMpPlanWarp = 2, kMpFirstDrain = 4, kMpDrainWarps = 8, kMpGatherWarps = 6;
 constexpr int kMpTable = 128;                // table entries that a CTA keeps in shared memory
 __host__ __device__ constexpr int mp_threads(bool placed) { return 32 * (kMpFirstDrain + kMpDrainWarps + (placed ? 0 : kMpGatherWarps - 1)); }
-constexpr int kMpSlots = 4, kMpMaxStages = 8;
+constexpr int kMpSlots = 4, kMpMaxStages = 12;
 constexpr int kMpTmemCols = 512;
 constexpr int kMpScaleCol = 2 * kMpTile;     // behind the two accumulators: scales of two steps, 8 + 16 columns each
 constexpr int kMpScaleCols = 24;
@@ -238,6 +238,17 @@ static_assert(offsetof(MpSmem, limit) == offsetof(MpSmem, dead) + 8, "wait_limit
 constexpr int kMpFixed = (int)((sizeof(MpSmem) + 127) / 128 * 128);
 constexpr int kMpSmemMax = 227 * 1024, kMpSmemMin = 116 * 1024;  // one CTA to an SM: each takes all of tensor memory
 
+// A step in the ring: weights, their scales, token rows, their scales.  Steps lie one behind the other, each as long as its item's
+// tile needs, and start again at 0 where the next does not fit: who fills and who reads work out the same places.
+__host__ __device__ constexpr uint32_t mp_step_bytes(int rows, int halves) {
+  return kMpABytes + kMpAScaleBytes + rows * (kMpStepChunks * kMxChunk / 2) + halves * kMpAScaleBytes;
+}
+__device__ __forceinline__ uint32_t mp_next_place(uint32_t& head, uint32_t bytes, uint32_t ring) {
+  const uint32_t at = head + bytes <= ring ? head : 0;
+  head = at + bytes;
+  return at;
+}
+
 struct MpParams {
   const slicemoe_mx4_mat* mats;
   const uint8_t* codes;
@@ -248,13 +259,15 @@ struct MpParams {
   const int *first, *list;             // of the placed rows
   const uint8_t *t_codes, *t_scale;
   int E, N, K, gated, T, k, x_per_pair;
-  int tile, stages;      // most tokens of a tile here, a multiple of 16; steps of the ring
+  int tile;              // most tokens of a tile here, a multiple of 16
+  int stages, ring;      // steps that may be under way, and the bytes that they share
   int row_blocks;
 };
 
-__device__ __forceinline__ uint64_t mp_desc(uint32_t addr, uint32_t lead, uint32_t stride) {  // no swizzle
-  return (uint64_t)((addr & 0x3FFFF) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(stride >> 4) << 32 | (uint64_t)1 << 46;
-}
+// Operand descriptors without swizzle: 8 rows x 16 bytes one after the other, 128 bytes on to the next eight rows (operands and scales
+// alike), `lead` bytes to the next 16 bytes of a row.  The upper half is the same for all.
+constexpr uint32_t kMpDescHigh = (128 >> 4) | 1u << 14;
+__device__ __forceinline__ uint64_t mp_desc(uint32_t low) { return (uint64_t)kMpDescHigh << 32 | low; }
 // E2M1 x E2M1, E8M0 scales, M 128, N tokens.  Bits 29 and 4: which pair of the four scale bytes, see mp_mma.
 __device__ __forceinline__ uint32_t mp_idesc(int n) {
   return (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | (1u << 23) | ((uint32_t)(kMxRows >> 4) << 24);
@@ -300,7 +313,10 @@ __device__ __forceinline__ void mp_cp16(uint32_t dst, const void* src, uint32_t 
 __device__ __forceinline__ bool mp_wait(const void* bar, uint32_t parity, MpSmem* s, unsigned* status) {
   return __all_sync(0xffffffffu, mbar_wait(smem_u32(bar), parity, &s->dead, status));
 }
-__device__ __forceinline__ float mp_silu(float v) { return v / (1.0f + expf(-v)); }
+// silu(g) u.  __expf(-g) is off by (2 + 1.2 |g|) 2^-23, which enters with the weight of e^-g / (1 + e^-g); |silu(g)| (2 + 1.2 |g|) times
+// that weight stays below 1.3 |g|: an error of 1.3 x 2^-23 |g u|, no more than that of the sums behind g and u (each of at least
+// 32 products).  __fdividef adds 2 ulp, and gives 0 for e^-g above 2^126, where the quotient is below 2^-119.
+__device__ __forceinline__ float mp_gated(float g, float u) { return __fdividef(g, 1.0f + __expf(-g)) * u; }
 
 template <class O>
 __device__ __forceinline__ uint32_t mp_pack2(float a, float b) {
@@ -318,7 +334,6 @@ __global__ void __launch_bounds__(mp_threads(PLACED), 1) mp_product_kernel(const
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int chunks = mx_chunks(p.K), atoms = mx_atoms(p.K), steps = (chunks + kMpStepChunks - 1) / kMpStepChunks;
   const int halves = (p.tile + 127) >> 7;  // scale blocks of 128 tokens
-  const uint32_t b_bytes = p.tile * (kMpStepChunks * kMxChunk / 2), stage_bytes = kMpABytes + kMpAScaleBytes + b_bytes + halves * kMpAScaleBytes;
   const uint32_t ring = smem_u32(mp_smem) + kMpFixed;
   unsigned* status = &p.head->status;
 
@@ -460,31 +475,44 @@ __global__ void __launch_bounds__(mp_threads(PLACED), 1) mp_product_kernel(const
       if (++slot == kMpSlots) slot = 0, turn ^= 1u;
     }
   } else if (warp == kMpWeightWarp) {
-    // ---- weights ----
-    uint32_t slot = 0, turn = 0, st = 0, ph = 0, filled = 0;
+    // ---- weights, and placed tiles ----
+    // Lane l keeps where the last step of barrier l lies.  A step may overwrite what the steps before it, up to the newest that it
+    // overlaps, have left behind: that one's products are waited for.
+    uint32_t slot = 0, turn = 0, st = 0, fill = 0, head = 0, filled = 0;
+    uint32_t my_at = 0, my_end = 0, my_fill = 0;  // my_end 0: none yet
     const bool bring = p.head->extra_arrivals == 0;
     if constexpr (PLACED) asm volatile("fence.proxy.async;" ::: "memory");  // the tiles were written by ordinary stores
     bool ok = true;
     while (ok && (ok = mp_wait(&s->item_full[slot], turn, s, status))) {
       const MpItem item = s->item[slot];
       if (item.n < 0) break;
+      const uint32_t bytes = mp_step_bytes(item.rows, halves);
       for (int i = 0; i < steps; ++i) {
-        if (!(ok = mp_wait(&s->free_[st], ph ^ 1u, s, status))) break;
+        const uint32_t at = mp_next_place(head, bytes, p.ring);
+        const uint32_t age = (uint32_t)lane < st ? st - lane : st + p.stages - lane;  // steps ago; of this barrier's own last: stages
+        const bool over = lane < p.stages && my_end > 0 && (age == (uint32_t)p.stages || (my_at < at + bytes && at < my_end));
+        const uint32_t newest = __reduce_min_sync(0xffffffffu, over ? age : 0xffffu);
+        if (newest != 0xffffu) {
+          const uint32_t b = st >= newest ? st - newest : st + p.stages - newest;
+          if (!(ok = mp_wait(&s->free_[b], __shfl_sync(0xffffffffu, my_fill, b) & 1u, s, status))) break;
+        }
         const int c = min(kMpStepChunks, chunks - i * kMpStepChunks), a = (c + 1) >> 1;
         if (bring && mp_elect()) {
-          const uint32_t dst = ring + st * stage_bytes, bar = smem_u32(&s->full_a[st]);
+          const uint32_t dst = ring + at, bar = smem_u32(&s->full_a[st]);
           const uint32_t t_bytes = PLACED ? c * item.rows * (kMxChunk / 2) : 0, ts_bytes = PLACED ? a * halves * kMxAtomBytes : 0;
           mbar_arrive_expect_tx(bar, c * kMxChunkBytes + a * kMxAtomBytes + t_bytes + ts_bytes);
           mp_bulk(dst, item.codes + (size_t)i * kMpABytes, c * kMxChunkBytes, bar);
           mp_bulk(dst + kMpABytes, item.scale + (size_t)i * kMpAScaleBytes, a * kMxAtomBytes, bar);
           if constexpr (PLACED) {
-            mp_bulk(dst + kMpABytes + kMpAScaleBytes, item.t_codes + (size_t)i * item.rows * (kMpStepChunks * kMxChunk / 2), t_bytes, bar);
-            mp_bulk(dst + kMpABytes + kMpAScaleBytes + b_bytes, item.t_scale + (size_t)i * halves * kMpAScaleBytes, ts_bytes, bar);
+            const uint32_t t_dst = dst + kMpABytes + kMpAScaleBytes;
+            mp_bulk(t_dst, item.t_codes + (size_t)i * item.rows * (kMpStepChunks * kMxChunk / 2), t_bytes, bar);
+            mp_bulk(t_dst + item.rows * (kMpStepChunks * kMxChunk / 2), item.t_scale + (size_t)i * halves * kMpAScaleBytes, ts_bytes, bar);
           }
         }
         __syncwarp();
+        if ((uint32_t)lane == st) my_at = at, my_end = at + bytes, my_fill = fill;
         ++filled;
-        if (++st == (uint32_t)p.stages) st = 0, ph ^= 1u;
+        if (++st == (uint32_t)p.stages) st = 0, ++fill;
       }
       if (!ok) break;
       if (lane == 0) mbar_arrive(smem_u32(&s->item_free[slot]));
@@ -501,32 +529,45 @@ __global__ void __launch_bounds__(mp_threads(PLACED), 1) mp_product_kernel(const
     }
   } else if (warp == kMpMmaWarp) {
     // ---- products ----
-    uint32_t slot = 0, turn = 0, st = 0, ph = 0, acc = 0, acc_ph = 0, flip = 0;
+    uint32_t slot = 0, turn = 0, st = 0, ph = 0, acc = 0, acc_ph = 0, flip = 0, head = 0;
     bool ok = true;
     while (ok && (ok = mp_wait(&s->item_full[slot], turn, s, status))) {
-      const int n = s->item[slot].n, rows = s->item[slot].rows;
+      // By way of a shuffle the compiler knows that these are the same in all lanes, and keeps what follows from them on the uniform
+      // datapath, where the tensor instructions take their operands from.  (A step's twelve instructions took the issuing thread 700
+      // clocks with descriptors made in ordinary registers, more than the weights take to arrive.)
+      const int n = __shfl_sync(0xffffffffu, s->item[slot].n, 0), rows = __shfl_sync(0xffffffffu, s->item[slot].rows, 0);
       if (n < 0) break;
       const uint32_t idesc = mp_idesc((n + 15) & ~15), d = tmem + acc * kMpTile;
-      const int blocks = (n + 127) >> 7;
+      const bool wide = n > 128;
+      const uint32_t b_bytes = rows * (kMpStepChunks * kMxChunk / 2), bytes = mp_step_bytes(rows, halves);
       if (!(ok = mp_wait(&s->acc_free[acc], acc_ph ^ 1u, s, status))) break;
       mp_fence_after();
       for (int i = 0; i < steps; ++i) {
         if (!(ok = mp_wait(&s->full_a[st], ph, s, status))) break;
         if (!PLACED && !(ok = mp_wait(&s->full_b[st], ph, s, status))) break;
         mp_fence_after();
-        const int c = min(kMpStepChunks, chunks - i * kMpStepChunks), a = (c + 1) >> 1;
+        const int c = chunks - i * kMpStepChunks;  // chunks of the step, if below four
+        const uint32_t at = ring + mp_next_place(head, bytes, p.ring);
         if (mp_elect()) {
-          const uint32_t at = ring + st * stage_bytes, b_at = at + kMpABytes + kMpAScaleBytes, bs_at = b_at + b_bytes;
+          const uint32_t b_at = at + kMpABytes + kMpAScaleBytes;
+          const uint32_t la = (at >> 4) + ((kMxRows * 16 >> 4) << 16), lb = (b_at >> 4) + ((uint32_t)rows << 16);
+          const uint32_t lsa = (at + kMpABytes) >> 4, lsb = (b_at + b_bytes) >> 4, next = halves * (kMxAtomBytes >> 4);
           const uint32_t sa = tmem + kMpScaleCol + flip * kMpScaleCols, sb = sa + 8;
-          for (int j = 0; j < a; ++j) {
-            mp_copy_scales(sa + 4 * j, mp_desc(at + kMpABytes + j * kMxAtomBytes, 0, 128));
-            for (int h = 0; h < blocks; ++h) mp_copy_scales(sb + 8 * j + 4 * h, mp_desc(bs_at + (j * halves + h) * kMxAtomBytes, 0, 128));
+          mp_copy_scales(sa, mp_desc(lsa));
+          mp_copy_scales(sb, mp_desc(lsb));
+          if (wide) mp_copy_scales(sb + 4, mp_desc(lsb + (kMxAtomBytes >> 4)));
+          if (c > 2) {
+            mp_copy_scales(sa + 4, mp_desc(lsa + (kMxAtomBytes >> 4)));
+            mp_copy_scales(sb + 8, mp_desc(lsb + next));
+            if (wide) mp_copy_scales(sb + 12, mp_desc(lsb + next + (kMxAtomBytes >> 4)));
           }
-          for (int j = 0; j < c; ++j) {
-            const uint32_t half = (uint32_t)(j & 1) * 2u;
-            mp_mma(d, mp_desc(at + j * kMxChunkBytes, kMxRows * 16, 128), mp_desc(b_at + j * rows * 32, rows * 16, 128),
-                   idesc | half << 29 | half << 4, sa + 4 * (j >> 1), sb + 8 * (j >> 1), (i | j) != 0);
-          }
+#pragma unroll
+          for (int j = 0; j < kMpStepChunks; ++j)
+            if (j < c) {
+              constexpr uint32_t kHigh = 2u << 29 | 2u << 4;  // the upper two of the four scale bytes
+              mp_mma(d, mp_desc(la + j * (kMxChunkBytes >> 4)), mp_desc(lb + j * 2 * rows), j & 1 ? idesc | kHigh : idesc, sa + 4 * (j >> 1),
+                     sb + 8 * (j >> 1), (uint32_t)(i | j));
+            }
           mp_commit(smem_u32(&s->free_[st]));
           if (i == steps - 1) mp_commit(smem_u32(&s->acc_full[acc]));
         }
@@ -564,7 +605,7 @@ __global__ void __launch_bounds__(mp_threads(PLACED), 1) mp_product_kernel(const
         if (next == me) {
           if (!(ok = mp_wait(&s->free_[st], ph ^ 1u, s, status))) break;
           const int c = min(kMpStepChunks, chunks - i * kMpStepChunks), a = (c + 1) >> 1;
-          const uint32_t dst = ring + st * stage_bytes + kMpABytes + kMpAScaleBytes, sdst = dst + b_bytes;
+          const uint32_t dst = ring + st * mp_step_bytes(p.tile, halves) + kMpABytes + kMpAScaleBytes, sdst = dst + p.tile * (kMpStepChunks * kMxChunk / 2);
           // scales: a word of four per row and 128 values, bytes beyond the row's end cleared.  All of a lane's loads are under way
           // before the first is used (one after the other they took longer than everything else: 16 us an item, not 2)
           constexpr int kRows = kMpTile / 32, kWords = kMpStepChunks / 2;
@@ -638,14 +679,28 @@ __global__ void __launch_bounds__(mp_threads(PLACED), 1) mp_product_kernel(const
         }
         if constexpr (GATED) {
           // lanes 0 to 15 hold gate, 16 to 31 up of the same columns of the result: of two tokens, the lower lanes take the first
-          const bool hi = lane & 16;
+          const bool hi = lane & 16, odd = lane & 1;
           const int col = rb * 64 + quarter * 16 + (lane & 15);
+          float h[8];
 #pragma unroll
-          for (int i = 0; i < 16; i += 2) {
-            const float v0 = __uint_as_float(r[i]), v1 = __uint_as_float(r[i + 1]);
+          for (int i = 0; i < 8; ++i) {
+            const float v0 = __uint_as_float(r[2 * i]), v1 = __uint_as_float(r[2 * i + 1]);
             const float got = __shfl_xor_sync(0xffffffffu, hi ? v0 : v1, 16);
-            const float g = hi ? got : v0, u = hi ? v1 : got;
-            if (c0 + i + (hi ? 1 : 0) < n && col < p.N) out[(size_t)(hi ? pr[i + 1] : pr[i]) * p.N + col] = mx_from_float<O>(mp_silu(g) * u);
+            h[i] = mp_gated(hi ? got : v0, hi ? v1 : got);
+          }
+          if (sizeof(O) == 2 && (p.N & 1) == 0) {  // two columns of one token to a lane
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+              const float got = __shfl_xor_sync(0xffffffffu, odd ? h[i] : h[i + 1], 1);
+              const int lo = odd ? pr[2 * i + 2] : pr[2 * i], up = odd ? pr[2 * i + 3] : pr[2 * i + 1];
+              const int token = c0 + 2 * i + (odd ? 2 : 0) + (hi ? 1 : 0);
+              if (token < n && col < p.N)
+                *reinterpret_cast<uint32_t*>(out + (size_t)(hi ? up : lo) * p.N + (col & ~1)) = mp_pack2<O>(odd ? got : h[i], odd ? h[i + 1] : got);
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              if (c0 + 2 * i + (hi ? 1 : 0) < n && col < p.N) out[(size_t)(hi ? pr[2 * i + 1] : pr[2 * i]) * p.N + col] = mx_from_float<O>(h[i]);
           }
         } else {
           const int col = rb * kMxRows + quarter * 32 + lane;
@@ -681,9 +736,6 @@ __global__ void __launch_bounds__(mp_threads(PLACED), 1) mp_product_kernel(const
   if (warp == kMpMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kMpTmemCols) : "memory");
 }
 
-static int mp_stage_bytes(int tile) {
-  return kMpABytes + kMpAScaleBytes + tile * (kMpStepChunks * kMxChunk / 2) + (tile + 127) / 128 * kMpAScaleBytes;
-}
 template <class O, bool GATED, bool PLACED>
 static int mp_launch(const MpParams& p, int items, cudaStream_t st) {
   static bool attr_set[64];
@@ -696,7 +748,7 @@ static int mp_launch(const MpParams& p, int items, cudaStream_t st) {
     SM_CUDA_TRY(cudaDeviceGetAttribute(&sm_count[dev], cudaDevAttrMultiProcessorCount, dev));
     attr_set[dev] = true;
   }
-  const int smem = kMpFixed + p.stages * mp_stage_bytes(p.tile);
+  const int smem = kMpFixed + p.ring;
   return mx_launch(mp_product_kernel<O, GATED, PLACED>, dim3(items < sm_count[dev] ? items : sm_count[dev]), mp_threads(PLACED),
                    (size_t)(smem > kMpSmemMin ? smem : kMpSmemMin), st, MpParams(p));
 }
@@ -751,8 +803,13 @@ extern "C" int slicemoe_mx4_product(const slicemoe_mx4_mat* mats, int n_experts,
   p.k = k;
   p.x_per_pair = x_per_pair;
   p.tile = mp_tile(T);
-  p.stages = (kMpSmemMax - kMpFixed) / mp_stage_bytes(p.tile);
-  if (p.stages > kMpMaxStages) p.stages = kMpMaxStages;
+  p.stages = kMpMaxStages;
+  p.ring = kMpSmemMax - kMpFixed;
+  if (pairs <= kMpInline) {  // steps of one size, whose places the gatherers know from their barrier
+    const int step = (int)mp_step_bytes(p.tile, (p.tile + 127) / 128);
+    if (p.stages > p.ring / step) p.stages = p.ring / step;
+    p.ring = p.stages * step;
+  }
   p.row_blocks = mx_row_blocks(N, gated);
   const int64_t tiles = (int64_t)pairs / p.tile + (pairs < E ? pairs : E), items = tiles * p.row_blocks;
   if (items > INT32_MAX) return SLICEMOE_E_UNSUPPORTED;
