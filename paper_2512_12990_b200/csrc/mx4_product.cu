@@ -41,8 +41,8 @@ __host__ __device__ inline MpTiles mp_tiles(int rows, int tile) {
 // An expert has at most T rows where no token names one twice: wider tiles would only take room from the ring.
 __host__ __device__ inline int mp_tile(int T) { return T >= kMpTile ? kMpTile : (T + 15) & ~15; }
 
-// Workspace: header; ranks of the pairs among the block's of their expert, and the blocks' counts; rows before each expert, the pairs by
-// expert; token rows in the operand layout.  Every part grows with each argument, so that a workspace serves smaller calls.
+// Workspace: header; ranks of the pairs among the block's of their expert, and the blocks' counts; rows, tiles and tiles' rows before each
+// expert; the pairs by expert; token rows in the operand layout.  Every part grows with each argument, so that a workspace serves smaller calls.
 struct MpLayout {
   size_t rank, hist, first, list, scale, codes, total;
   int blocks;
@@ -55,7 +55,7 @@ __host__ __device__ inline MpLayout mp_layout(int T, int k, int E, int K) {
   l.rank = 256;
   l.hist = l.rank + up(pairs * sizeof(int));
   l.first = l.hist + up((size_t)l.blocks * E * sizeof(int));
-  l.list = l.first + up((E + 1) * sizeof(int));
+  l.list = l.first + up((size_t)3 * (E + 1) * sizeof(int));
   l.scale = l.list + up(pairs * sizeof(int));
   l.codes = l.scale + up((size_t)tiles * 2 * mx_atoms(K) * kMxAtomBytes);
   l.total = l.codes + up((size_t)(pairs + 16 * tiles) * mx_chunks(K) * (kMxChunk / 2));
@@ -121,7 +121,7 @@ struct MpPlaceParams {
   const int32_t* ids;  // NULL: all of expert 0, in order
   const int *rank, *hist;
   const uint8_t *codes, *scale;
-  int *first, *list;
+  int *first, *list;    // first: [3][E + 1], rows, tiles and tiles' rows before an expert
   uint8_t *t_codes, *t_scale;
   int pairs, E, blocks, chunk, tile, k, x_per_pair, K;
 };
@@ -159,10 +159,10 @@ __global__ void __launch_bounds__(kMpPlaceThreads) mp_place_kernel(const MpPlace
     padded += total;
     if (e < p.E) {
       s_first[e] = f, s_before[e] = before, s_count[e] = count, s_tile[e] = o, s_row[e] = r;
-      if (blockIdx.x == 0) p.first[e] = f;
+      if (blockIdx.x == 0) p.first[e] = f, p.first[p.E + 1 + e] = o, p.first[2 * (p.E + 1) + e] = r;
     }
   }
-  if (blockIdx.x == 0 && tid == 0) p.first[p.E] = rows;
+  if (blockIdx.x == 0 && tid == 0) p.first[p.E] = rows, p.first[2 * p.E + 1] = tiles;
   __syncthreads();
   const int chunks = mx_chunks(p.K), atoms = mx_atoms(p.K), pieces = 2 * chunks, kbytes = p.K >> 1, halves = (p.tile + 127) >> 7;
   for (int i = warp * 8; i < p.chunk; i += kMpPlaceThreads / 32 * 8) {
@@ -231,8 +231,8 @@ struct __align__(16) MpSmem {
   int first[kMpMaxExperts + 1];  // rows before an expert
   int tiles[kMpMaxExperts + 1];  // tiles before it
   int padded[kMpMaxExperts];     // rows of the tiles before it
+  uint32_t place[kMpMaxStages];  // where the steps under way begin
   int list[kMpInline];
-  int sums[32];
 };
 static_assert(offsetof(MpSmem, limit) == offsetof(MpSmem, dead) + 8, "wait_limit()");
 constexpr int kMpFixed = (int)((sizeof(MpSmem) + 127) / 128 * 128);
@@ -259,6 +259,7 @@ struct MpParams {
   const int *first, *list;             // of the placed rows
   const uint8_t *t_codes, *t_scale;
   int E, N, K, gated, T, k, x_per_pair;
+  uint32_t k_inverse;    // ceil(2^32 / k), for k > 1
   int tile;              // most tokens of a tile here, a multiple of 16
   int stages, ring;      // steps that may be under way, and the bytes that they share
   int row_blocks;
@@ -338,105 +339,110 @@ __global__ void __launch_bounds__(mp_threads(PLACED), 1) mp_product_kernel(const
   unsigned* status = &p.head->status;
 
   mx_dep_launch();
-  if (tid == 0) {
-    for (int i = 0; i < kMpMaxStages; ++i) {
-      mbar_init(smem_u32(&s->full_a[i]), 1);
-      mbar_init(smem_u32(&s->full_b[i]), 1);
-      mbar_init(smem_u32(&s->free_[i]), 1);
-    }
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(smem_u32(&s->acc_full[i]), 1);
-      mbar_init(smem_u32(&s->acc_free[i]), kMpDrainWarps);
-    }
-    for (int i = 0; i < kMpSlots; ++i) {
-      mbar_init(smem_u32(&s->item_full[i]), 1);
-      mbar_init(smem_u32(&s->item_free[i]), 2 + (PLACED ? 0 : kMpGatherWarps) + kMpDrainWarps);
-    }
-    mbar_init(smem_u32(&s->drain), 1);
-    s->dead = 0;
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  }
   if (warp == kMpMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s->tmem)), "r"(kMpTmemCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
-  // the table does not change between launches: it is read while the kernel before is still at work
-  if (p.E <= kMpTable) {
+  } else if (warp == kMpPlanWarp) {
+    if constexpr (!PLACED)
+      for (int e = lane; e <= p.E; e += 32) s->first[e] = 0;
+    if (lane == 0) {
+      s->dead = 0;
+      s->limit = p.head->wait_cycles ? p.head->wait_cycles : kWaitCycles;
+    }
+  } else if (warp >= kMpFirstDrain && warp < kMpFirstDrain + 2) {
+    // one barrier to a thread: they lie one behind the other in the order of MpSmem
+    const int i = tid - 32 * kMpFirstDrain;
+    constexpr int kRing = 3 * kMpMaxStages, kAll = kRing + 4 + 2 * kMpSlots + 1;
+    static_assert(kAll <= 64 && offsetof(MpSmem, drain) == 8 * (kAll - 1), "barriers");
+    int arrivals = 1;
+    if (i >= kRing + 2 && i < kRing + 4) arrivals = kMpDrainWarps;
+    if (i >= kRing + 4 + kMpSlots && i < kRing + 4 + 2 * kMpSlots) arrivals = 2 + (PLACED ? 0 : kMpGatherWarps) + kMpDrainWarps;
+    if (i < kAll) mbar_init(smem_u32(&s->full_a[0] + i), arrivals);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  } else if (warp >= kMpFirstDrain + 4 && warp < kMpFirstDrain + 8 && p.E <= kMpTable) {
+    // the table does not change between launches: it is read while the kernel before is still at work
     constexpr int kWords = sizeof(slicemoe_mx4_mat) / 8;
-    for (int i = tid; i < p.E * kWords; i += kThreads)
+    for (int i = tid - 32 * (kMpFirstDrain + 4); i < p.E * kWords; i += 128)
       reinterpret_cast<unsigned long long*>(s->mats)[i] = __ldg(reinterpret_cast<const unsigned long long*>(p.mats) + i);
   }
-  for (int e = tid; e <= p.E; e += kThreads) s->first[e] = 0;
-  mx_dep_wait();
-  if (tid == 0) s->limit = p.head->wait_cycles ? p.head->wait_cycles : kWaitCycles;
-  int rank = 0, e_mine = -1;
-  if constexpr (PLACED) {
-    for (int e = tid; e <= p.E; e += kThreads) s->first[e] = __ldcg(p.first + e);
-  } else if (p.ids) {  // few pairs: by expert, here
-    const int pairs = p.T * p.k;
-    __syncthreads();
-    e_mine = tid < pairs ? __ldcg(p.ids + tid) : -1;
-    if ((unsigned)e_mine >= (unsigned)p.E) e_mine = -1;
-    if (tid < pairs && e_mine < 0 && blockIdx.x == 0) atomicOr(status, (unsigned)SLICEMOE_STATUS_BAD_EXPERT_ID);
-    // in the order of the list, warp after warp: all CTAs must deal the same pairs to the same tiles
-    const unsigned same = __match_any_sync(0xffffffffu, e_mine), lower = same & ((1u << lane) - 1u);
-    for (int w = 0; w * 32 < pairs; ++w) {
-      if (warp == w && e_mine >= 0) rank = s->first[e_mine] + __popc(lower);
-      __syncwarp();
-      if (warp == w && e_mine >= 0 && lower == 0) s->first[e_mine] += __popc(same);
-      __syncthreads();
-    }
-  } else {
-    for (int e = tid; e <= p.E; e += kThreads) s->first[e] = e ? p.T : 0;
-  }
-  __syncthreads();
-  int tiles = 0, rows = 0, padded = 0;
-  for (int e0 = 0; e0 < p.E; e0 += kThreads) {
-    const int e = e0 + tid;
-    int count = 0, total;
-    if (e < p.E) count = !PLACED && p.ids ? s->first[e] : s->first[e + 1] - s->first[e];
-    const MpTiles t = mp_tiles(count, p.tile);
-    const int o = tiles + mp_scan<kThreads>(t.n, s->sums, &total);
-    tiles += total;
-    if (e < p.E) s->tiles[e] = o;
-    if constexpr (PLACED) {
-      const int r = padded + mp_scan<kThreads>(t.n * t.each, s->sums, &total);
-      padded += total;
-      if (e < p.E) s->padded[e] = r;
-    } else if (p.ids) {
-      const int f = rows + mp_scan<kThreads>(count, s->sums, &total);  // its barriers lie between the reads of first[] and this write
-      rows += total;
-      if (e < p.E) s->first[e] = f;
-    }
-  }
-  if constexpr (!PLACED) {
-    if (p.ids) {
-      if (tid == 0) s->first[p.E] = rows;
-      __syncthreads();
-      if (e_mine >= 0) s->list[s->first[e_mine] + rank] = tid;
-    }
-  }
-  const int total_items = tiles * p.row_blocks;
   mp_fence_before();
   __syncthreads();
   mp_fence_after();
   const uint32_t tmem = s->tmem;
 
   if (warp == kMpPlanWarp) {
-    // ---- which item is next, and its rows ----
+    // ---- the plan: rows by expert, then which item is next, and its rows.  One warp does it, the others wait for their first item: with
+    // few pairs that is a chain of latencies which barriers of the whole CTA would only lengthen ----
+    int at = blockIdx.x / p.row_blocks, rest = blockIdx.x - at * p.row_blocks;  // an item's place among the tiles
+    const int at_step = gridDim.x / p.row_blocks, rest_step = gridDim.x - at_step * p.row_blocks;
+    mx_dep_wait();
+    if constexpr (PLACED) {
+      for (int e = lane; e <= p.E; e += 32) {
+        s->first[e] = __ldcg(p.first + e);
+        s->tiles[e] = __ldcg(p.first + p.E + 1 + e);
+        if (e < p.E) s->padded[e] = __ldcg(p.first + 2 * (p.E + 1) + e);
+      }
+    } else if (p.ids) {
+      const int pairs = p.T * p.k;
+      int* where = &s->pair[0][0];  // not in use yet: expert and rank of a pair
+      static_assert(kMpSlots * kMpTile >= kMpInline, "room for the pairs");
+      // ranks in the order of the list: all CTAs must deal the same pairs to the same tiles
+      for (int i0 = 0; i0 < pairs; i0 += 128) {
+        int id[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) id[q] = i0 + 32 * q + lane < pairs ? __ldcg(p.ids + i0 + 32 * q + lane) : -2;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          if (i0 + 32 * q >= pairs) break;
+          const bool named = (unsigned)id[q] < (unsigned)p.E;
+          const unsigned same = __match_any_sync(0xffffffffu, named ? id[q] : -1), lower = same & ((1u << lane) - 1u);
+          const int rank = named ? s->first[id[q]] + __popc(lower) : 0;
+          __syncwarp();
+          if (named && lower == 0) s->first[id[q]] += __popc(same);
+          __syncwarp();
+          where[i0 + 32 * q + lane] = named ? id[q] << 16 | rank : -1;
+          if (!named && id[q] != -2 && blockIdx.x == 0) atomicOr(status, (unsigned)SLICEMOE_STATUS_BAD_EXPERT_ID);
+        }
+      }
+      __syncwarp();
+      int before = 0;  // rows in the low half, tiles in the high one
+      for (int e0 = 0; e0 < p.E; e0 += 32) {
+        const int e = e0 + lane, count = e < p.E ? s->first[e] : 0;
+        const int v = count | (count + p.tile - 1 >= p.tile + p.tile ? (count + p.tile - 1) / p.tile : count > 0) << 16;
+        int inc = v;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+          const int o = __shfl_up_sync(0xffffffffu, inc, off);
+          if (lane >= off) inc += o;
+        }
+        const int here = before + inc - v;
+        if (e < p.E) s->first[e] = here & 0xffff, s->tiles[e] = here >> 16;
+        before += __shfl_sync(0xffffffffu, inc, 31);
+      }
+      if (lane == 0) s->first[p.E] = before & 0xffff, s->tiles[p.E] = before >> 16;
+      __syncwarp();
+      for (int i = lane; i < pairs; i += 32) {
+        const int v = where[i];
+        if (v >= 0) s->list[s->first[v >> 16] + (v & 0xffff)] = i;
+      }
+    } else if (lane == 0) {
+      s->first[0] = s->tiles[0] = 0;
+      s->first[1] = p.T;
+      s->tiles[1] = (p.T + p.tile - 1) / p.tile;
+    }
+    __syncwarp();
+    const int total_tiles = s->tiles[p.E];
     uint32_t slot = 0, turn = 0;
-    bool ok = true;
-    for (int it = blockIdx.x;; it += gridDim.x) {
-      ok = mp_wait(&s->item_free[slot], turn ^ 1u, s, status);
-      if (!ok) break;
-      if (it >= total_items) {
+    for (;; at += at_step, rest += rest_step) {
+      if (rest >= p.row_blocks) rest -= p.row_blocks, ++at;
+      if (!mp_wait(&s->item_free[slot], turn ^ 1u, s, status)) break;
+      if (at >= total_tiles) {
         if (lane == 0) s->item[slot].n = -1;
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&s->item_full[slot]));
         break;
       }
-      // its expert: the last one whose first tile is not above the item's (in tiles of all row blocks); two steps of 32 lanes
-      const int at = it / p.row_blocks;
+      // its expert: the last one whose first tile is not above the item's; two steps of 32 lanes
       int e = 32 * (__popc(__ballot_sync(0xffffffffu, lane * 32 < p.E && s->tiles[lane * 32] <= at)) - 1);
       e += __popc(__ballot_sync(0xffffffffu, e + lane < p.E && s->tiles[e + lane] <= at)) - 1;
       const slicemoe_mx4_mat m = p.E <= kMpTable ? s->mats[e] : p.mats[e];
@@ -445,9 +451,10 @@ __global__ void __launch_bounds__(mp_threads(PLACED), 1) mp_product_kernel(const
         continue;
       }
       // of an expert's items a row block's tiles come one after the other: its weights are in L2 for all but the first
-      const int first = s->first[e], count = s->first[e + 1] - first, local = it - s->tiles[e] * p.row_blocks;
-      const MpTiles tt = mp_tiles(count, p.tile);
-      const int rb = local / tt.n, t = local - rb * tt.n, r0 = t * tt.each, n = min(tt.each, count - r0);
+      const int first = s->first[e], count = s->first[e + 1] - first, e_tile = s->tiles[e];
+      const MpTiles tt = count <= p.tile ? MpTiles{1, (count + 15) & ~15} : mp_tiles(count, p.tile);
+      const int local = (at - e_tile) * p.row_blocks + rest, rb = tt.n == 1 ? local : local / tt.n, t = local - rb * tt.n;
+      const int r0 = t * tt.each, n = min(tt.each, count - r0);
       for (int i = lane; i < n; i += 32) {
         const int at = first + r0 + i;
         if constexpr (PLACED) {
@@ -455,7 +462,7 @@ __global__ void __launch_bounds__(mp_threads(PLACED), 1) mp_product_kernel(const
         } else {
           const int pair = p.ids ? s->list[at] : at;
           s->pair[slot][i] = pair;
-          s->row[slot][i] = p.x_per_pair ? pair : pair / p.k;
+          s->row[slot][i] = p.x_per_pair ? pair : (int)__umulhi((uint32_t)pair, p.k_inverse);
         }
       }
       if (lane == 0) {
@@ -467,7 +474,7 @@ __global__ void __launch_bounds__(mp_threads(PLACED), 1) mp_product_kernel(const
         item->rb = rb;
         if constexpr (PLACED) {
           item->t_codes = p.t_codes + (size_t)(s->padded[e] + r0) * chunks * (kMxChunk / 2);
-          item->t_scale = p.t_scale + (size_t)(s->tiles[e] + t) * atoms * halves * kMxAtomBytes;
+          item->t_scale = p.t_scale + (size_t)(e_tile + t) * atoms * halves * kMxAtomBytes;
         }
       }
       __syncwarp();
@@ -475,81 +482,87 @@ __global__ void __launch_bounds__(mp_threads(PLACED), 1) mp_product_kernel(const
       if (++slot == kMpSlots) slot = 0, turn ^= 1u;
     }
   } else if (warp == kMpWeightWarp) {
-    // ---- weights, and placed tiles ----
-    // Lane l keeps where the last step of barrier l lies.  A step may overwrite what the steps before it, up to the newest that it
-    // overlaps, have left behind: that one's products are waited for.
-    uint32_t slot = 0, turn = 0, st = 0, fill = 0, head = 0, filled = 0;
-    uint32_t my_at = 0, my_end = 0, my_fill = 0;  // my_end 0: none yet
-    const bool bring = p.head->extra_arrivals == 0;
-    if constexpr (PLACED) asm volatile("fence.proxy.async;" ::: "memory");  // the tiles were written by ordinary stores
-    bool ok = true;
-    while (ok && (ok = mp_wait(&s->item_full[slot], turn, s, status))) {
-      const MpItem item = s->item[slot];
-      if (item.n < 0) break;
-      const uint32_t bytes = mp_step_bytes(item.rows, halves);
-      for (int i = 0; i < steps; ++i) {
-        const uint32_t at = mp_next_place(head, bytes, p.ring);
-        const uint32_t age = (uint32_t)lane < st ? st - lane : st + p.stages - lane;  // steps ago; of this barrier's own last: stages
-        const bool over = lane < p.stages && my_end > 0 && (age == (uint32_t)p.stages || (my_at < at + bytes && at < my_end));
-        const uint32_t newest = __reduce_min_sync(0xffffffffu, over ? age : 0xffffu);
-        if (newest != 0xffffu) {
-          const uint32_t b = st >= newest ? st - newest : st + p.stages - newest;
-          if (!(ok = mp_wait(&s->free_[b], __shfl_sync(0xffffffffu, my_fill, b) & 1u, s, status))) break;
-        }
-        const int c = min(kMpStepChunks, chunks - i * kMpStepChunks), a = (c + 1) >> 1;
-        if (bring && mp_elect()) {
-          const uint32_t dst = ring + at, bar = smem_u32(&s->full_a[st]);
-          const uint32_t t_bytes = PLACED ? c * item.rows * (kMxChunk / 2) : 0, ts_bytes = PLACED ? a * halves * kMxAtomBytes : 0;
-          mbar_arrive_expect_tx(bar, c * kMxChunkBytes + a * kMxAtomBytes + t_bytes + ts_bytes);
-          mp_bulk(dst, item.codes + (size_t)i * kMpABytes, c * kMxChunkBytes, bar);
-          mp_bulk(dst + kMpABytes, item.scale + (size_t)i * kMpAScaleBytes, a * kMxAtomBytes, bar);
-          if constexpr (PLACED) {
-            const uint32_t t_dst = dst + kMpABytes + kMpAScaleBytes;
-            mp_bulk(t_dst, item.t_codes + (size_t)i * item.rows * (kMpStepChunks * kMxChunk / 2), t_bytes, bar);
-            mp_bulk(t_dst + item.rows * (kMpStepChunks * kMxChunk / 2), item.t_scale + (size_t)i * halves * kMpAScaleBytes, ts_bytes, bar);
-          }
-        }
-        __syncwarp();
-        if ((uint32_t)lane == st) my_at = at, my_end = at + bytes, my_fill = fill;
-        ++filled;
-        if (++st == (uint32_t)p.stages) st = 0, ++fill;
+    // ---- weights, and placed tiles.  One thread, and the compiler knows it: addresses stay on the uniform datapath ----
+    if (mp_elect()) {
+      uint32_t slot = 0, turn = 0, st = 0, head = 0;
+      uint32_t live = 0, old = 0, old_ph = 0;  // steps not known to be consumed, the oldest one's barrier
+      uint32_t filled = 0;
+      const bool bring = p.head->extra_arrivals == 0;
+      if constexpr (PLACED) {
+        mx_dep_wait();
+        asm volatile("fence.proxy.async;" ::: "memory");  // the tiles were written by ordinary stores
       }
-      if (!ok) break;
-      if (lane == 0) mbar_arrive(smem_u32(&s->item_free[slot]));
-      if (++slot == kMpSlots) slot = 0, turn ^= 1u;
-    }
-    if (bring) {  // what is on its way lands before the CTA ends, also where another role has given up
-      const uint32_t mine = min(filled, (uint32_t)p.stages);
-      for (uint32_t i = 0; i < mine; ++i) {
-        const uint32_t f = filled - 1 - i, b = f % p.stages, par = (f / p.stages) & 1u;
+      bool ok = true;
+      while (ok && (ok = mbar_wait(smem_u32(&s->item_full[slot]), turn, &s->dead, status))) {
+        const MpItem item = s->item[slot];
+        if (item.n < 0) break;
+        const uint32_t bytes = mp_step_bytes(item.rows, halves), t_step = item.rows * (kMpStepChunks * kMxChunk / 2);
+        for (int i = 0; i < steps; ++i) {
+          uint32_t at;
+          for (;;) {
+            at = head + bytes <= (uint32_t)p.ring ? head : 0;
+            if (live == 0) break;
+            // what is live lies in [tail, head), or in [tail, ...) and [0, head) where it has started again at 0
+            const uint32_t tail = s->place[old];
+            const bool room = head > tail ? at == head || bytes <= tail : at == head && head + bytes <= tail;
+            if (room && live < (uint32_t)p.stages) break;
+            if (!(ok = mbar_wait(smem_u32(&s->free_[old]), old_ph, &s->dead, status))) break;
+            --live;
+            if (++old == (uint32_t)p.stages) old = 0, old_ph ^= 1u;
+          }
+          if (!ok) break;
+          head = at + bytes;
+          s->place[st] = at;
+          ++live;
+          if (bring) {
+            const int c = min(kMpStepChunks, chunks - i * kMpStepChunks), a = (c + 1) >> 1;
+            const uint32_t dst = ring + at, bar = smem_u32(&s->full_a[st]);
+            const uint32_t t_bytes = PLACED ? c * item.rows * (kMxChunk / 2) : 0, ts_bytes = PLACED ? a * halves * kMxAtomBytes : 0;
+            mbar_arrive_expect_tx(bar, c * kMxChunkBytes + a * kMxAtomBytes + t_bytes + ts_bytes);
+            mp_bulk(dst, item.codes + (size_t)i * kMpABytes, c * kMxChunkBytes, bar);
+            mp_bulk(dst + kMpABytes, item.scale + (size_t)i * kMpAScaleBytes, a * kMxAtomBytes, bar);
+            if constexpr (PLACED) {
+              const uint32_t t_dst = dst + kMpABytes + kMpAScaleBytes;
+              mp_bulk(t_dst, item.t_codes + (size_t)i * t_step, t_bytes, bar);
+              mp_bulk(t_dst + t_step, item.t_scale + (size_t)i * halves * kMpAScaleBytes, ts_bytes, bar);
+            }
+            ++filled;
+          }
+          if (++st == (uint32_t)p.stages) st = 0;
+        }
+        if (!ok) break;
+        mbar_arrive(smem_u32(&s->item_free[slot]));
+        if (++slot == kMpSlots) slot = 0, turn ^= 1u;
+      }
+      // what is on its way lands before the CTA ends, also where another role has given up
+      for (uint32_t i = 1; i <= min(filled, (uint32_t)p.stages); ++i) {
+        const uint32_t f = filled - i, b = f % p.stages, par = (f / p.stages) & 1u;
         const long long t0 = clock64();
         while (!mbar_try(smem_u32(&s->full_a[b]), par) && clock64() - t0 < 4000000ll) {
         }
       }
     }
+    __syncwarp();
   } else if (warp == kMpMmaWarp) {
-    // ---- products ----
-    uint32_t slot = 0, turn = 0, st = 0, ph = 0, acc = 0, acc_ph = 0, flip = 0, head = 0;
-    bool ok = true;
-    while (ok && (ok = mp_wait(&s->item_full[slot], turn, s, status))) {
-      // By way of a shuffle the compiler knows that these are the same in all lanes, and keeps what follows from them on the uniform
-      // datapath, where the tensor instructions take their operands from.  (A step's twelve instructions took the issuing thread 700
-      // clocks with descriptors made in ordinary registers, more than the weights take to arrive.)
-      const int n = __shfl_sync(0xffffffffu, s->item[slot].n, 0), rows = __shfl_sync(0xffffffffu, s->item[slot].rows, 0);
-      if (n < 0) break;
-      const uint32_t idesc = mp_idesc((n + 15) & ~15), d = tmem + acc * kMpTile;
-      const bool wide = n > 128;
-      const uint32_t b_bytes = rows * (kMpStepChunks * kMxChunk / 2), bytes = mp_step_bytes(rows, halves);
-      if (!(ok = mp_wait(&s->acc_free[acc], acc_ph ^ 1u, s, status))) break;
-      mp_fence_after();
-      for (int i = 0; i < steps; ++i) {
-        if (!(ok = mp_wait(&s->full_a[st], ph, s, status))) break;
-        if (!PLACED && !(ok = mp_wait(&s->full_b[st], ph, s, status))) break;
+    // ---- products.  One thread too.  (With descriptors made in ordinary registers a step's twelve instructions took it 700 clocks, more
+    // than the weights take to arrive; 285 with warp-wide waits.) ----
+    if (mp_elect()) {
+      uint32_t slot = 0, turn = 0, st = 0, ph = 0, acc = 0, acc_ph = 0, flip = 0, head = 0;
+      bool ok = true;
+      while (ok && (ok = mbar_wait(smem_u32(&s->item_full[slot]), turn, &s->dead, status))) {
+        const int n = s->item[slot].n, rows = s->item[slot].rows;
+        if (n < 0) break;
+        const uint32_t idesc = mp_idesc((n + 15) & ~15), d = tmem + acc * kMpTile;
+        const bool wide = n > 128;
+        const uint32_t b_bytes = rows * (kMpStepChunks * kMxChunk / 2), bytes = mp_step_bytes(rows, halves);
+        if (!(ok = mbar_wait(smem_u32(&s->acc_free[acc]), acc_ph ^ 1u, &s->dead, status))) break;
         mp_fence_after();
-        const int c = chunks - i * kMpStepChunks;  // chunks of the step, if below four
-        const uint32_t at = ring + mp_next_place(head, bytes, p.ring);
-        if (mp_elect()) {
-          const uint32_t b_at = at + kMpABytes + kMpAScaleBytes;
+        for (int i = 0; i < steps; ++i) {
+          if (!(ok = mbar_wait(smem_u32(&s->full_a[st]), ph, &s->dead, status))) break;
+          if (!PLACED && !(ok = mbar_wait(smem_u32(&s->full_b[st]), ph, &s->dead, status))) break;
+          mp_fence_after();
+          const int c = chunks - i * kMpStepChunks;  // chunks of the step, if below four
+          const uint32_t at = ring + mp_next_place(head, bytes, p.ring), b_at = at + kMpABytes + kMpAScaleBytes;
           const uint32_t la = (at >> 4) + ((kMxRows * 16 >> 4) << 16), lb = (b_at >> 4) + ((uint32_t)rows << 16);
           const uint32_t lsa = (at + kMpABytes) >> 4, lsb = (b_at + b_bytes) >> 4, next = halves * (kMxAtomBytes >> 4);
           const uint32_t sa = tmem + kMpScaleCol + flip * kMpScaleCols, sb = sa + 8;
@@ -569,23 +582,22 @@ __global__ void __launch_bounds__(mp_threads(PLACED), 1) mp_product_kernel(const
                      sb + 8 * (j >> 1), (uint32_t)(i | j));
             }
           mp_commit(smem_u32(&s->free_[st]));
-          if (i == steps - 1) mp_commit(smem_u32(&s->acc_full[acc]));
+          flip ^= 1u;
+          if (++st == (uint32_t)p.stages) st = 0, ph ^= 1u;
         }
-        __syncwarp();
-        flip ^= 1u;
-        if (++st == (uint32_t)p.stages) st = 0, ph ^= 1u;
+        if (!ok) break;
+        mp_commit(smem_u32(&s->acc_full[acc]));
+        mbar_arrive(smem_u32(&s->item_free[slot]));
+        if (++slot == kMpSlots) slot = 0, turn ^= 1u;
+        if (acc ^= 1u; acc == 0) acc_ph ^= 1u;
       }
-      if (!ok) break;
-      if (lane == 0) mbar_arrive(smem_u32(&s->item_free[slot]));
-      if (++slot == kMpSlots) slot = 0, turn ^= 1u;
-      if (acc ^= 1u; acc == 0) acc_ph ^= 1u;
+      // every instruction issued is done before tensor memory is given back
+      mp_commit(smem_u32(&s->drain));
+      const long long t0 = clock64();
+      while (!mbar_try(smem_u32(&s->drain), 0) && clock64() - t0 < 4000000ll) {
+      }
     }
-    // every instruction issued is done before tensor memory is given back
-    if (mp_elect()) mp_commit(smem_u32(&s->drain));
     __syncwarp();
-    const long long t0 = clock64();
-    while (!mbar_try(smem_u32(&s->drain), 0) && clock64() - t0 < 4000000ll) {
-    }
   } else if (warp < kMpFirstDrain || warp >= kMpFirstDrain + kMpDrainWarps) {
     // ---- token rows, where they are not placed: the warps bring the steps in turn ----
     if constexpr (!PLACED) {
@@ -597,6 +609,7 @@ __global__ void __launch_bounds__(mp_threads(PLACED), 1) mp_product_kernel(const
     int next = 0;  // whose turn the step is
     bool ok = true;
     const int pitch = 4 * atoms, kbytes = p.K >> 1;
+    mx_dep_wait();
     while (ok && (ok = mp_wait(&s->item_full[slot], turn, s, status))) {
       const int n = s->item[slot].n;
       if (n < 0) break;
@@ -661,6 +674,7 @@ __global__ void __launch_bounds__(mp_threads(PLACED), 1) mp_product_kernel(const
     uint32_t slot = 0, turn = 0, acc = 0, acc_ph = 0;
     bool ok = true;
     O* out = static_cast<O*>(p.out);
+    mx_dep_wait();
     while (ok && (ok = mp_wait(&s->item_full[slot], turn, s, status))) {
       const int n = s->item[slot].n, rb = s->item[slot].rb;
       if (n < 0) break;
@@ -801,7 +815,8 @@ extern "C" int slicemoe_mx4_product(const slicemoe_mx4_mat* mats, int n_experts,
   p.gated = gated;
   p.T = T;
   p.k = k;
-  p.x_per_pair = x_per_pair;
+  p.x_per_pair = x_per_pair || k == 1;
+  p.k_inverse = k > 1 ? (uint32_t)((0x100000000ull + k - 1) / k) : 0;
   p.tile = mp_tile(T);
   p.stages = kMpMaxStages;
   p.ring = kMpSmemMax - kMpFixed;
