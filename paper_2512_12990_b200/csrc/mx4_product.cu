@@ -24,8 +24,9 @@ struct MpHeader {
 constexpr int kMpMaxExperts = 1024;
 constexpr int64_t kMpMaxPairs = 1 << 24;
 constexpr int kMpTile = 224;         // most tokens of a tile
-constexpr int kMpInline = 512;       // pairs up to which the product's CTAs sort them and gather the rows themselves
-constexpr int kMpSortPairs = 4096;   // above: pairs of a block of the kernel that ranks them
+constexpr int kMpFew = 512;          // up to so many pairs, and
+constexpr int kMpResident = 96 * 1024;  // so many bytes of token rows, every CTA keeps all rows and plans for itself
+constexpr int kMpSortPairs = 4096;   // else: pairs of a block of the kernel that ranks them
 constexpr int kMpSortThreads = 1024, kMpPlaceThreads = 256;
 
 // An expert's rows are cut into as few tiles as they fit, of equal size (a multiple of 16).
@@ -199,10 +200,9 @@ __global__ void __launch_bounds__(kMpPlaceThreads) mp_place_kernel(const MpPlace
 
 // ---- the product ----------------------------------------------------------------------------------------------------
 constexpr int kMpStepChunks = 4;             // chunks of 64 values a step
-// Warps: weights (and tiles), products, plan; then, from the fourth on, eight that drain; the rows' gatherers are the third and those behind.
-constexpr int kMpWeightWarp = 0, kMpMmaWarp = 1, kMpPlanWarp = 2, kMpFirstDrain = 4, kMpDrainWarps = 8, kMpGatherWarps = 6;
+constexpr int kMpWeightWarp = 0, kMpMmaWarp = 1, kMpPlanWarp = 2, kMpFirstDrain = 4, kMpDrainWarps = 8;  // warp 3 helps to lay out resident rows
+constexpr int kMpThreads = 32 * (kMpFirstDrain + kMpDrainWarps);
 constexpr int kMpTable = 128;                // table entries that a CTA keeps in shared memory
-__host__ __device__ constexpr int mp_threads(bool placed) { return 32 * (kMpFirstDrain + kMpDrainWarps + (placed ? 0 : kMpGatherWarps - 1)); }
 constexpr int kMpSlots = 4, kMpMaxStages = 12;
 constexpr int kMpTmemCols = 512;
 constexpr int kMpScaleCol = 2 * kMpTile;     // behind the two accumulators: scales of two steps, 8 + 16 columns each
@@ -213,27 +213,28 @@ constexpr int kMpABytes = kMpStepChunks * kMxChunkBytes, kMpAScaleBytes = kMpSte
 struct MpItem {
   const uint8_t *codes, *scale;      // the row block's weights
   const uint8_t *t_codes, *t_scale;  // the placed tile
-  int n;         // tokens; < 0: no more items
+  int n;         // columns, a multiple of 16; < 0: no more items
   int rows;      // rows of the tile as it lies, a multiple of 16
   int rb;        // row block
-  int pad_;
+  uint32_t groups;  // the sixteens of columns that hold pairs of the item
 };
 struct __align__(16) MpSmem {
-  unsigned long long full_a[kMpMaxStages], full_b[kMpMaxStages], free_[kMpMaxStages];
-  unsigned long long acc_full[2], acc_free[2], item_full[kMpSlots], item_free[kMpSlots], drain;
+  unsigned long long full[kMpMaxStages], free_[kMpMaxStages];
+  unsigned long long acc_full[2], acc_free[2], item_full[kMpSlots], item_free[kMpSlots], resident, drain;
   uint32_t tmem;
   int pad0;
   int dead, pad1;
   unsigned long long limit;  // 8 bytes behind dead
   MpItem item[kMpSlots];
-  int pair[kMpSlots][kMpTile], row[kMpSlots][kMpTile];
+  alignas(16) int pair[kMpSlots][kMpTile];  // of a column; -1: none; read four at a time
   slicemoe_mx4_mat mats[kMpTable];
   int first[kMpMaxExperts + 1];  // rows before an expert
   int tiles[kMpMaxExperts + 1];  // tiles before it
   int padded[kMpMaxExperts];     // rows of the tiles before it
   uint32_t place[kMpMaxStages];  // where the steps under way begin
-  int list[kMpInline];
+  int key[kMpFew], tile[kMpFew]; // of a pair, and of a tile, where the CTA plans for itself: expert, and how often the token named it before << 16
 };
+static_assert(offsetof(MpSmem, pair) % 16 == 0 && kMpTile % 4 == 0 && offsetof(MpSmem, mats) % 8 == 0, "alignment");
 static_assert(offsetof(MpSmem, limit) == offsetof(MpSmem, dead) + 8, "wait_limit()");
 constexpr int kMpFixed = (int)((sizeof(MpSmem) + 127) / 128 * 128);
 constexpr int kMpSmemMax = 227 * 1024, kMpSmemMin = 116 * 1024;  // one CTA to an SM: each takes all of tensor memory
@@ -260,7 +261,8 @@ struct MpParams {
   const uint8_t *t_codes, *t_scale;
   int E, N, K, gated, T, k, x_per_pair;
   uint32_t k_inverse;    // ceil(2^32 / k), for k > 1
-  int tile;              // most tokens of a tile here, a multiple of 16
+  int tile;              // most tokens of a tile, a multiple of 16; resident: all rows
+  int resident;          // bytes of resident rows and their scales
   int stages, ring;      // steps that may be under way, and the bytes that they share
   int row_blocks;
 };
@@ -307,9 +309,6 @@ __device__ __forceinline__ void mp_bulk(uint32_t dst, const void* src, uint32_t 
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
                : "memory");
 }
-__device__ __forceinline__ void mp_cp16(uint32_t dst, const void* src, uint32_t bytes) {  // bytes 0: zeros
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-}
 // By a whole warp; every lane gets the same answer.
 __device__ __forceinline__ bool mp_wait(const void* bar, uint32_t parity, MpSmem* s, unsigned* status) {
   return __all_sync(0xffffffffu, mbar_wait(smem_u32(bar), parity, &s->dead, status));
@@ -327,15 +326,17 @@ __device__ __forceinline__ uint32_t mp_pack2(float a, float b) {
   return w;
 }
 
+// PLACED: token rows come tile by tile, as mp_place_kernel has laid them out.  Else all rows of the call are resident in shared memory, and
+// an item's tile is all of them: the tensor instruction takes hardly longer for the columns that no pair of the item uses, and
+// nothing has to be gathered.
 template <class O, bool GATED, bool PLACED>
-__global__ void __launch_bounds__(mp_threads(PLACED), 1) mp_product_kernel(const MpParams p) {
-  constexpr int kThreads = mp_threads(PLACED);
+__global__ void __launch_bounds__(kMpThreads, 1) mp_product_kernel(const MpParams p) {
   extern __shared__ __align__(128) uint8_t mp_smem[];
   MpSmem* s = reinterpret_cast<MpSmem*>(mp_smem);
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int chunks = mx_chunks(p.K), atoms = mx_atoms(p.K), steps = (chunks + kMpStepChunks - 1) / kMpStepChunks;
   const int halves = (p.tile + 127) >> 7;  // scale blocks of 128 tokens
-  const uint32_t ring = smem_u32(mp_smem) + kMpFixed;
+  const uint32_t rows_at = smem_u32(mp_smem) + kMpFixed, ring = rows_at + p.resident;
   unsigned* status = &p.head->status;
 
   mx_dep_launch();
@@ -343,8 +344,6 @@ __global__ void __launch_bounds__(mp_threads(PLACED), 1) mp_product_kernel(const
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s->tmem)), "r"(kMpTmemCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   } else if (warp == kMpPlanWarp) {
-    if constexpr (!PLACED)
-      for (int e = lane; e <= p.E; e += 32) s->first[e] = 0;
     if (lane == 0) {
       s->dead = 0;
       s->limit = p.head->wait_cycles ? p.head->wait_cycles : kWaitCycles;
@@ -352,12 +351,13 @@ __global__ void __launch_bounds__(mp_threads(PLACED), 1) mp_product_kernel(const
   } else if (warp >= kMpFirstDrain && warp < kMpFirstDrain + 2) {
     // one barrier to a thread: they lie one behind the other in the order of MpSmem
     const int i = tid - 32 * kMpFirstDrain;
-    constexpr int kRing = 3 * kMpMaxStages, kAll = kRing + 4 + 2 * kMpSlots + 1;
+    constexpr int kRing = 2 * kMpMaxStages, kAll = kRing + 4 + 2 * kMpSlots + 2;
     static_assert(kAll <= 64 && offsetof(MpSmem, drain) == 8 * (kAll - 1), "barriers");
     int arrivals = 1;
     if (i >= kRing + 2 && i < kRing + 4) arrivals = kMpDrainWarps;
-    if (i >= kRing + 4 + kMpSlots && i < kRing + 4 + 2 * kMpSlots) arrivals = 2 + (PLACED ? 0 : kMpGatherWarps) + kMpDrainWarps;
-    if (i < kAll) mbar_init(smem_u32(&s->full_a[0] + i), arrivals);
+    if (i >= kRing + 4 + kMpSlots && i < kRing + 4 + 2 * kMpSlots) arrivals = 2 + kMpDrainWarps;
+    if (i == kAll - 2) arrivals = kMpDrainWarps + 1;
+    if (i < kAll) mbar_init(smem_u32(&s->full[0] + i), arrivals);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   } else if (warp >= kMpFirstDrain + 4 && warp < kMpFirstDrain + 8 && p.E <= kMpTable) {
     // the table does not change between launches: it is read while the kernel before is still at work
@@ -365,16 +365,41 @@ __global__ void __launch_bounds__(mp_threads(PLACED), 1) mp_product_kernel(const
     for (int i = tid - 32 * (kMpFirstDrain + 4); i < p.E * kWords; i += 128)
       reinterpret_cast<unsigned long long*>(s->mats)[i] = __ldg(reinterpret_cast<const unsigned long long*>(p.mats) + i);
   }
+  const int pairs = p.T * p.k;
+  if (!PLACED && pairs > 32)
+    for (int e = tid; e < p.E; e += kMpThreads) s->first[e] = 0;
   mp_fence_before();
   __syncthreads();
   mp_fence_after();
   const uint32_t tmem = s->tmem;
 
+  if (!PLACED && pairs > 32) {
+    // more pairs than lanes: all warps look at them.  A tile of an expert takes one pair of a token; first[] counts its tiles
+    mx_dep_wait();
+    for (int i = tid; i < pairs; i += kMpThreads) {
+      int e = p.ids ? __ldcg(p.ids + i) : 0;
+      if ((unsigned)e >= (unsigned)p.E) {
+        e = -1;
+        if (blockIdx.x == 0) atomicOr(status, (unsigned)SLICEMOE_STATUS_BAD_EXPERT_ID);
+      }
+      s->tile[i] = e;
+    }
+    __syncthreads();
+    for (int i = tid; i < pairs; i += kMpThreads) {
+      const int e = s->tile[i], t0 = p.k > 1 ? (int)__umulhi((uint32_t)i, p.k_inverse) * p.k : i;
+      int before = 0;
+      for (int j = t0; j < i; ++j) before += s->tile[j] == e;
+      s->key[i] = e < 0 ? -1 : e | before << 16;
+      if (e >= 0) atomicMax(&s->first[e], before + 1);
+    }
+    __syncthreads();
+  }
   if (warp == kMpPlanWarp) {
     // ---- the plan: rows by expert, then which item is next, and its rows.  One warp does it, the others wait for their first item: with
     // few pairs that is a chain of latencies which barriers of the whole CTA would only lengthen ----
     int at = blockIdx.x / p.row_blocks, rest = blockIdx.x - at * p.row_blocks;  // an item's place among the tiles
     const int at_step = gridDim.x / p.row_blocks, rest_step = gridDim.x - at_step * p.row_blocks;
+    int total_tiles = 0;
     mx_dep_wait();
     if constexpr (PLACED) {
       for (int e = lane; e <= p.E; e += 32) {
@@ -382,56 +407,39 @@ __global__ void __launch_bounds__(mp_threads(PLACED), 1) mp_product_kernel(const
         s->tiles[e] = __ldcg(p.first + p.E + 1 + e);
         if (e < p.E) s->padded[e] = __ldcg(p.first + 2 * (p.E + 1) + e);
       }
-    } else if (p.ids) {
-      const int pairs = p.T * p.k;
-      int* where = &s->pair[0][0];  // not in use yet: expert and rank of a pair
-      static_assert(kMpSlots * kMpTile >= kMpInline, "room for the pairs");
-      // ranks in the order of the list: all CTAs must deal the same pairs to the same tiles
-      for (int i0 = 0; i0 < pairs; i0 += 128) {
-        int id[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) id[q] = i0 + 32 * q + lane < pairs ? __ldcg(p.ids + i0 + 32 * q + lane) : -2;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          if (i0 + 32 * q >= pairs) break;
-          const bool named = (unsigned)id[q] < (unsigned)p.E;
-          const unsigned same = __match_any_sync(0xffffffffu, named ? id[q] : -1), lower = same & ((1u << lane) - 1u);
-          const int rank = named ? s->first[id[q]] + __popc(lower) : 0;
-          __syncwarp();
-          if (named && lower == 0) s->first[id[q]] += __popc(same);
-          __syncwarp();
-          where[i0 + 32 * q + lane] = named ? id[q] << 16 | rank : -1;
-          if (!named && id[q] != -2 && blockIdx.x == 0) atomicOr(status, (unsigned)SLICEMOE_STATUS_BAD_EXPERT_ID);
+    } else if (pairs <= 32) {
+      int e = -1;
+      if (lane < pairs) {
+        e = p.ids ? __ldcg(p.ids + lane) : 0;
+        if ((unsigned)e >= (unsigned)p.E) {
+          e = -1;
+          if (blockIdx.x == 0) atomicOr(status, (unsigned)SLICEMOE_STATUS_BAD_EXPERT_ID);
         }
       }
-      __syncwarp();
-      int before = 0;  // rows in the low half, tiles in the high one
+      const unsigned lower = (1u << lane) - 1u, token = p.k > 1 ? ~0u << (__umulhi((uint32_t)lane, p.k_inverse) * p.k) : ~0u << lane;
+      const unsigned same = __match_any_sync(0xffffffffu, e);  // by all lanes, whatever they hold
+      const int key = e < 0 ? -1 : e | __popc(same & lower & token) << 16;
+      const unsigned alike = __match_any_sync(0xffffffffu, key);
+      const bool leads = key >= 0 && (alike & lower) == 0;
+      const unsigned all = __ballot_sync(0xffffffffu, leads);
+      s->key[lane] = key;
+      if (leads) s->tile[__popc(all & lower)] = key;
+      total_tiles = __popc(all);
+    } else {
       for (int e0 = 0; e0 < p.E; e0 += 32) {
         const int e = e0 + lane, count = e < p.E ? s->first[e] : 0;
-        const int v = count | (count + p.tile - 1 >= p.tile + p.tile ? (count + p.tile - 1) / p.tile : count > 0) << 16;
-        int inc = v;
+        int inc = count;
 #pragma unroll
         for (int off = 1; off < 32; off <<= 1) {
           const int o = __shfl_up_sync(0xffffffffu, inc, off);
           if (lane >= off) inc += o;
         }
-        const int here = before + inc - v;
-        if (e < p.E) s->first[e] = here & 0xffff, s->tiles[e] = here >> 16;
-        before += __shfl_sync(0xffffffffu, inc, 31);
+        for (int m = 0; m < count; ++m) s->tile[total_tiles + inc - count + m] = e | m << 16;
+        total_tiles += __shfl_sync(0xffffffffu, inc, 31);
       }
-      if (lane == 0) s->first[p.E] = before & 0xffff, s->tiles[p.E] = before >> 16;
-      __syncwarp();
-      for (int i = lane; i < pairs; i += 32) {
-        const int v = where[i];
-        if (v >= 0) s->list[s->first[v >> 16] + (v & 0xffff)] = i;
-      }
-    } else if (lane == 0) {
-      s->first[0] = s->tiles[0] = 0;
-      s->first[1] = p.T;
-      s->tiles[1] = (p.T + p.tile - 1) / p.tile;
     }
     __syncwarp();
-    const int total_tiles = s->tiles[p.E];
+    if constexpr (PLACED) total_tiles = s->tiles[p.E];
     uint32_t slot = 0, turn = 0;
     for (;; at += at_step, rest += rest_step) {
       if (rest >= p.row_blocks) rest -= p.row_blocks, ++at;
@@ -442,40 +450,56 @@ __global__ void __launch_bounds__(mp_threads(PLACED), 1) mp_product_kernel(const
         if (lane == 0) mbar_arrive(smem_u32(&s->item_full[slot]));
         break;
       }
-      // its expert: the last one whose first tile is not above the item's; two steps of 32 lanes
-      int e = 32 * (__popc(__ballot_sync(0xffffffffu, lane * 32 < p.E && s->tiles[lane * 32] <= at)) - 1);
-      e += __popc(__ballot_sync(0xffffffffu, e + lane < p.E && s->tiles[e + lane] <= at)) - 1;
+      int e, key = 0;
+      if constexpr (PLACED) {  // the last expert whose first tile is not above the item's; two steps of 32 lanes
+        e = 32 * (__popc(__ballot_sync(0xffffffffu, lane * 32 < p.E && s->tiles[lane * 32] <= at)) - 1);
+        e += __popc(__ballot_sync(0xffffffffu, e + lane < p.E && s->tiles[e + lane] <= at)) - 1;
+      } else {
+        key = s->tile[at];
+        e = key & 0xffff;
+      }
       const slicemoe_mx4_mat m = p.E <= kMpTable ? s->mats[e] : p.mats[e];
       if (!m.codes || !m.scale || m.N != p.N || m.K != p.K || (m.gated != 0) != GATED) {
         if (lane == 0) atomicOr(status, (unsigned)SLICEMOE_STATUS_BAD_EXPERT_ID);
         continue;
       }
-      // of an expert's items a row block's tiles come one after the other: its weights are in L2 for all but the first
-      const int first = s->first[e], count = s->first[e + 1] - first, e_tile = s->tiles[e];
-      const MpTiles tt = count <= p.tile ? MpTiles{1, (count + 15) & ~15} : mp_tiles(count, p.tile);
-      const int local = (at - e_tile) * p.row_blocks + rest, rb = tt.n == 1 ? local : local / tt.n, t = local - rb * tt.n;
-      const int r0 = t * tt.each, n = min(tt.each, count - r0);
-      for (int i = lane; i < n; i += 32) {
-        const int at = first + r0 + i;
-        if constexpr (PLACED) {
-          s->pair[slot][i] = __ldcg(p.list + at);
-        } else {
-          const int pair = p.ids ? s->list[at] : at;
-          s->pair[slot][i] = pair;
-          s->row[slot][i] = p.x_per_pair ? pair : (int)__umulhi((uint32_t)pair, p.k_inverse);
+      MpItem* item = &s->item[slot];
+      int rb = rest;
+      if constexpr (PLACED) {
+        // of an expert's items a row block's tiles come one after the other: its weights are in L2 for all but the first
+        const int first = s->first[e], count = s->first[e + 1] - first, e_tile = s->tiles[e];
+        const MpTiles tt = count <= p.tile ? MpTiles{1, (count + 15) & ~15} : mp_tiles(count, p.tile);
+        const int local = (at - e_tile) * p.row_blocks + rest;
+        rb = tt.n == 1 ? local : local / tt.n;
+        const int t = local - rb * tt.n, r0 = t * tt.each, n = min(tt.each, count - r0), n16 = (n + 15) & ~15;
+        for (int i = lane; i < n16; i += 32) s->pair[slot][i] = i < n ? __ldcg(p.list + first + r0 + i) : -1;
+        if (lane == 0) {
+          item->t_codes = p.t_codes + (size_t)(s->padded[e] + r0) * chunks * (kMxChunk / 2);
+          item->t_scale = p.t_scale + (size_t)(e_tile + t) * atoms * halves * kMxAtomBytes;
+          item->n = n16;
+          item->rows = tt.each;
+          item->groups = (1u << (n16 >> 4)) - 1u;
+        }
+      } else {
+        for (int i = lane; i < p.tile; i += 32) s->pair[slot][i] = -1;
+        __syncwarp();
+        uint32_t groups = 0;
+        for (int i = lane; i < pairs; i += 32)
+          if (s->key[i] == key) {
+            const int row = p.x_per_pair ? i : (int)__umulhi((uint32_t)i, p.k_inverse);
+            s->pair[slot][row] = i;
+            groups |= 1u << (row >> 4);
+          }
+        groups = __reduce_or_sync(0xffffffffu, groups);
+        if (lane == 0) {
+          item->n = item->rows = p.tile;
+          item->groups = groups;
         }
       }
       if (lane == 0) {
-        MpItem* item = &s->item[slot];
         item->codes = m.codes + (size_t)rb * chunks * kMxChunkBytes;
         item->scale = m.scale + (size_t)rb * atoms * kMxAtomBytes;
-        item->n = n;
-        item->rows = PLACED ? tt.each : p.tile;
         item->rb = rb;
-        if constexpr (PLACED) {
-          item->t_codes = p.t_codes + (size_t)(s->padded[e] + r0) * chunks * (kMxChunk / 2);
-          item->t_scale = p.t_scale + (size_t)(e_tile + t) * atoms * halves * kMxAtomBytes;
-        }
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&s->item_full[slot]));
@@ -496,7 +520,7 @@ __global__ void __launch_bounds__(mp_threads(PLACED), 1) mp_product_kernel(const
       while (ok && (ok = mbar_wait(smem_u32(&s->item_full[slot]), turn, &s->dead, status))) {
         const MpItem item = s->item[slot];
         if (item.n < 0) break;
-        const uint32_t bytes = mp_step_bytes(item.rows, halves), t_step = item.rows * (kMpStepChunks * kMxChunk / 2);
+        const uint32_t bytes = PLACED ? mp_step_bytes(item.rows, halves) : kMpABytes + kMpAScaleBytes, t_step = item.rows * (kMpStepChunks * kMxChunk / 2);
         for (int i = 0; i < steps; ++i) {
           uint32_t at;
           for (;;) {
@@ -516,7 +540,7 @@ __global__ void __launch_bounds__(mp_threads(PLACED), 1) mp_product_kernel(const
           ++live;
           if (bring) {
             const int c = min(kMpStepChunks, chunks - i * kMpStepChunks), a = (c + 1) >> 1;
-            const uint32_t dst = ring + at, bar = smem_u32(&s->full_a[st]);
+            const uint32_t dst = ring + at, bar = smem_u32(&s->full[st]);
             const uint32_t t_bytes = PLACED ? c * item.rows * (kMxChunk / 2) : 0, ts_bytes = PLACED ? a * halves * kMxAtomBytes : 0;
             mbar_arrive_expect_tx(bar, c * kMxChunkBytes + a * kMxAtomBytes + t_bytes + ts_bytes);
             mp_bulk(dst, item.codes + (size_t)i * kMpABytes, c * kMxChunkBytes, bar);
@@ -538,7 +562,7 @@ __global__ void __launch_bounds__(mp_threads(PLACED), 1) mp_product_kernel(const
       for (uint32_t i = 1; i <= min(filled, (uint32_t)p.stages); ++i) {
         const uint32_t f = filled - i, b = f % p.stages, par = (f / p.stages) & 1u;
         const long long t0 = clock64();
-        while (!mbar_try(smem_u32(&s->full_a[b]), par) && clock64() - t0 < 4000000ll) {
+        while (!mbar_try(smem_u32(&s->full[b]), par) && clock64() - t0 < 4000000ll) {
         }
       }
     }
@@ -548,23 +572,23 @@ __global__ void __launch_bounds__(mp_threads(PLACED), 1) mp_product_kernel(const
     // than the weights take to arrive; 285 with warp-wide waits.) ----
     if (mp_elect()) {
       uint32_t slot = 0, turn = 0, st = 0, ph = 0, acc = 0, acc_ph = 0, flip = 0, head = 0;
-      bool ok = true;
+      bool ok = PLACED || mbar_wait(smem_u32(&s->resident), 0, &s->dead, status);
       while (ok && (ok = mbar_wait(smem_u32(&s->item_full[slot]), turn, &s->dead, status))) {
         const int n = s->item[slot].n, rows = s->item[slot].rows;
         if (n < 0) break;
-        const uint32_t idesc = mp_idesc((n + 15) & ~15), d = tmem + acc * kMpTile;
+        const uint32_t idesc = mp_idesc(n), d = tmem + acc * kMpTile;
         const bool wide = n > 128;
-        const uint32_t b_bytes = rows * (kMpStepChunks * kMxChunk / 2), bytes = mp_step_bytes(rows, halves);
+        const uint32_t b_bytes = rows * (kMpStepChunks * kMxChunk / 2), bytes = PLACED ? mp_step_bytes(rows, halves) : kMpABytes + kMpAScaleBytes;
         if (!(ok = mbar_wait(smem_u32(&s->acc_free[acc]), acc_ph ^ 1u, &s->dead, status))) break;
         mp_fence_after();
         for (int i = 0; i < steps; ++i) {
-          if (!(ok = mbar_wait(smem_u32(&s->full_a[st]), ph, &s->dead, status))) break;
-          if (!PLACED && !(ok = mbar_wait(smem_u32(&s->full_b[st]), ph, &s->dead, status))) break;
+          if (!(ok = mbar_wait(smem_u32(&s->full[st]), ph, &s->dead, status))) break;
           mp_fence_after();
           const int c = chunks - i * kMpStepChunks;  // chunks of the step, if below four
-          const uint32_t at = ring + mp_next_place(head, bytes, p.ring), b_at = at + kMpABytes + kMpAScaleBytes;
+          const uint32_t at = ring + mp_next_place(head, bytes, p.ring), b_at = PLACED ? at + kMpABytes + kMpAScaleBytes : rows_at + i * b_bytes;
           const uint32_t la = (at >> 4) + ((kMxRows * 16 >> 4) << 16), lb = (b_at >> 4) + ((uint32_t)rows << 16);
-          const uint32_t lsa = (at + kMpABytes) >> 4, lsb = (b_at + b_bytes) >> 4, next = halves * (kMxAtomBytes >> 4);
+          const uint32_t s_at = PLACED ? b_at + b_bytes : rows_at + chunks * rows * (kMxChunk / 2) + i * halves * kMpAScaleBytes;
+          const uint32_t lsa = (at + kMpABytes) >> 4, lsb = s_at >> 4, next = halves * (kMxAtomBytes >> 4);
           const uint32_t sa = tmem + kMpScaleCol + flip * kMpScaleCols, sb = sa + 8;
           mp_copy_scales(sa, mp_desc(lsa));
           mp_copy_scales(sb, mp_desc(lsb));
@@ -598,90 +622,61 @@ __global__ void __launch_bounds__(mp_threads(PLACED), 1) mp_product_kernel(const
       }
     }
     __syncwarp();
-  } else if (warp < kMpFirstDrain || warp >= kMpFirstDrain + kMpDrainWarps) {
-    // ---- token rows, where they are not placed: the warps bring the steps in turn ----
-    if constexpr (!PLACED) {
-    const int me = warp < kMpFirstDrain ? 0 : warp - (kMpFirstDrain + kMpDrainWarps) + 1;
-    uint32_t slot = 0, turn = 0, st = 0, ph = 0;
-    // No more warps take turns than the ring has steps.  A warp's next step is then at most one round of the ring ahead of one that
-    // it has waited for, and the parity of a barrier tells it what it needs: with more it could be two rounds ahead.
-    const int gathers = min(kMpGatherWarps, p.stages);
-    int next = 0;  // whose turn the step is
-    bool ok = true;
-    const int pitch = 4 * atoms, kbytes = p.K >> 1;
-    mx_dep_wait();
-    while (ok && (ok = mp_wait(&s->item_full[slot], turn, s, status))) {
-      const int n = s->item[slot].n;
-      if (n < 0) break;
-      const int *rows = s->row[slot];
-      for (int i = 0; i < steps; ++i) {
-        if (next == me) {
-          if (!(ok = mp_wait(&s->free_[st], ph ^ 1u, s, status))) break;
-          const int c = min(kMpStepChunks, chunks - i * kMpStepChunks), a = (c + 1) >> 1;
-          const uint32_t dst = ring + st * mp_step_bytes(p.tile, halves) + kMpABytes + kMpAScaleBytes, sdst = dst + p.tile * (kMpStepChunks * kMxChunk / 2);
-          // scales: a word of four per row and 128 values, bytes beyond the row's end cleared.  All of a lane's loads are under way
-          // before the first is used (one after the other they took longer than everything else: 16 us an item, not 2)
-          constexpr int kRows = kMpTile / 32, kWords = kMpStepChunks / 2;
-          uint32_t w[kRows][kWords];
-#pragma unroll
-          for (int q = 0; q < kRows; ++q) {
-            const int r = q * 32 + lane;
-            const uint8_t* src = p.scale + (size_t)(r < n ? rows[r] : 0) * pitch + i * (2 * kMpStepChunks);
-#pragma unroll
-            for (int j = 0; j < kWords; ++j) w[q][j] = r < n && j < a ? __ldcg(reinterpret_cast<const uint32_t*>(src) + j) : 0u;
-          }
-          // codes: eight rows x four pieces of 16 bytes a step of the warp; a shared-memory write is eight rows side by side
-#pragma unroll 4
-          for (int r = lane & 7; r < n; r += 8) {
-            const uint8_t* src = p.codes + (size_t)rows[r] * kbytes;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const int piece = (lane >> 3) + 4 * h, at = i * (kMpStepChunks * kMxChunk / 2) + piece * 16;
-              if (piece < 2 * c) {
-                const bool in = at < kbytes;
-                mp_cp16(dst + (piece >> 1) * p.tile * 32 + (piece & 1) * p.tile * 16 + r * 16, in ? src + at : src, in ? 16u : 0u);
-              }
-            }
-          }
-#pragma unroll
-          for (int j = 0; j < kWords; ++j) {
-            const int left = (p.K >> 5) - (i * kWords + j) * 4;
-            const uint32_t mask = left < 4 ? (1u << (8 * max(left, 0))) - 1u : 0xffffffffu;
-#pragma unroll
-            for (int q = 0; q < kRows; ++q) {
-              const int r = q * 32 + lane;
-              if (r < n && j < a)
-                asm volatile("st.shared.b32 [%0], %1;" ::"r"(sdst + (j * halves + (q >> 2)) * kMxAtomBytes + lane * 16 + (q & 3) * 4), "r"(w[q][j] & mask)
-                             : "memory");
-            }
-          }
-          asm volatile("cp.async.wait_all;" ::: "memory");
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(&s->full_b[st]));
-        }
-        if (++next == gathers) next = 0;
-        if (++st == (uint32_t)p.stages) st = 0, ph ^= 1u;
-      }
-      if (!ok) break;
-      if (lane == 0) mbar_arrive(smem_u32(&s->item_free[slot]));
-      if (++slot == kMpSlots) slot = 0, turn ^= 1u;
-    }
-    }
   } else {
-    // ---- results: a warp reads 32 weight rows, 16 tokens at a time, every other sixteen ----
+    if constexpr (!PLACED) {
+      // ---- all rows of the call into the operand layout, eight rows x four pieces of 16 bytes at a time ----
+      mx_dep_wait();
+      const int rows = p.x_per_pair ? pairs : p.T, kbytes = p.K >> 1, pieces = 2 * chunks, scales = rows_at + chunks * p.tile * (kMxChunk / 2);
+      const int eights = (rows + 7) >> 3, quads = (pieces + 3) >> 2;
+      for (int i = warp - 3; i < eights * quads; i += kMpDrainWarps + 1) {
+        const int quad = i / eights, r = (i - quad * eights) * 8 + (lane & 7), q = quad * 4 + (lane >> 3);
+        if (r < rows && q < pieces) {  // beyond the row's end zeros; all of a lane's copies are under way at once
+          const uint8_t* src = p.codes + (size_t)r * kbytes;
+          const bool in = q * 16 < kbytes;
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(rows_at + (q * p.tile + r) * 16), "l"(in ? src + q * 16 : src),
+                       "r"(in ? 16u : 0u)
+                       : "memory");
+        }
+      }
+      constexpr int kStride = 32 * (kMpDrainWarps + 1), kAhead = 4;
+      for (int i0 = (warp - 3) * 32 + lane; i0 < rows * atoms; i0 += kAhead * kStride) {
+        uint32_t w[kAhead];
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a)
+          if (i0 + a * kStride < rows * atoms) w[a] = __ldcg(reinterpret_cast<const uint32_t*>(p.scale) + i0 + a * kStride);
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) {
+          const int i = i0 + a * kStride;
+          if (i >= rows * atoms) break;
+          const int r = i / atoms, j = i - r * atoms, left = (p.K >> 5) - 4 * j;
+          const uint32_t v = left < 4 ? w[a] & ((1u << (8 * left)) - 1u) : w[a];  // bytes beyond the row's end
+          asm volatile("st.shared.b32 [%0], %1;" ::"r"(scales + (j * halves + (r >> 7)) * kMxAtomBytes + (r & 31) * 16 + ((r >> 5) & 3) * 4), "r"(v) : "memory");
+        }
+      }
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&s->resident));
+    }
+    if (warp >= kMpFirstDrain) {
+    // ---- results: a warp reads 32 weight rows, 16 tokens at a time, every other sixteen that is in use ----
     const int quarter = warp & 3, half = (warp - kMpFirstDrain) >> 2;
     uint32_t slot = 0, turn = 0, acc = 0, acc_ph = 0;
     bool ok = true;
     O* out = static_cast<O*>(p.out);
     mx_dep_wait();
     while (ok && (ok = mp_wait(&s->item_full[slot], turn, s, status))) {
-      const int n = s->item[slot].n, rb = s->item[slot].rb;
-      if (n < 0) break;
+      const int rb = s->item[slot].rb;
+      uint32_t groups = s->item[slot].groups;
+      if (s->item[slot].n < 0) break;
       if (!(ok = mp_wait(&s->acc_full[acc], acc_ph, s, status))) break;
       mp_fence_after();
       const uint32_t d = tmem + ((uint32_t)(quarter * 32) << 16) + acc * kMpTile;
-      for (int c0 = 16 * half; c0 < n; c0 += 32) {
+      if (half) groups &= groups - 1u;
+      while (groups) {
+        const int c0 = 16 * (__ffs(groups) - 1);
+        groups &= groups - 1u;
+        groups &= groups - 1u;
         uint32_t r[16];
         mp_ld16(d + c0, r);
         const int4* pairs = reinterpret_cast<const int4*>(&s->pair[slot][c0]);
@@ -706,15 +701,14 @@ __global__ void __launch_bounds__(mp_threads(PLACED), 1) mp_product_kernel(const
 #pragma unroll
             for (int i = 0; i < 8; i += 2) {
               const float got = __shfl_xor_sync(0xffffffffu, odd ? h[i] : h[i + 1], 1);
-              const int lo = odd ? pr[2 * i + 2] : pr[2 * i], up = odd ? pr[2 * i + 3] : pr[2 * i + 1];
-              const int token = c0 + 2 * i + (odd ? 2 : 0) + (hi ? 1 : 0);
-              if (token < n && col < p.N)
-                *reinterpret_cast<uint32_t*>(out + (size_t)(hi ? up : lo) * p.N + (col & ~1)) = mp_pack2<O>(odd ? got : h[i], odd ? h[i + 1] : got);
+              const int lo = odd ? pr[2 * i + 2] : pr[2 * i], up = odd ? pr[2 * i + 3] : pr[2 * i + 1], pair = hi ? up : lo;
+              if (pair >= 0 && col < p.N)
+                *reinterpret_cast<uint32_t*>(out + (size_t)pair * p.N + (col & ~1)) = mp_pack2<O>(odd ? got : h[i], odd ? h[i + 1] : got);
             }
           } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-              if (c0 + 2 * i + (hi ? 1 : 0) < n && col < p.N) out[(size_t)(hi ? pr[2 * i + 1] : pr[2 * i]) * p.N + col] = mx_from_float<O>(h[i]);
+              if (const int pair = hi ? pr[2 * i + 1] : pr[2 * i]; pair >= 0 && col < p.N) out[(size_t)pair * p.N + col] = mx_from_float<O>(h[i]);
           }
         } else {
           const int col = rb * kMxRows + quarter * 32 + lane;
@@ -724,13 +718,13 @@ __global__ void __launch_bounds__(mp_threads(PLACED), 1) mp_product_kernel(const
             for (int i = 0; i < 16; i += 2) {
               const float v0 = __uint_as_float(r[i]), v1 = __uint_as_float(r[i + 1]);
               const float got = __shfl_xor_sync(0xffffffffu, hi ? v0 : v1, 1);
-              if (c0 + i + (hi ? 1 : 0) < n && col < p.N)
-                *reinterpret_cast<uint32_t*>(out + (size_t)(hi ? pr[i + 1] : pr[i]) * p.N + (col & ~1)) = mp_pack2<O>(hi ? got : v0, hi ? v1 : got);
+              if (const int pair = hi ? pr[i + 1] : pr[i]; pair >= 0 && col < p.N)
+                *reinterpret_cast<uint32_t*>(out + (size_t)pair * p.N + (col & ~1)) = mp_pack2<O>(hi ? got : v0, hi ? v1 : got);
             }
           } else {
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-              if (c0 + i < n && col < p.N) out[(size_t)pr[i] * p.N + col] = mx_from_float<O>(__uint_as_float(r[i]));
+              if (pr[i] >= 0 && col < p.N) out[(size_t)pr[i] * p.N + col] = mx_from_float<O>(__uint_as_float(r[i]));
           }
         }
       }
@@ -742,6 +736,7 @@ __global__ void __launch_bounds__(mp_threads(PLACED), 1) mp_product_kernel(const
       }
       if (++slot == kMpSlots) slot = 0, turn ^= 1u;
       if (acc ^= 1u; acc == 0) acc_ph ^= 1u;
+    }
     }
   }
   mp_fence_before();
@@ -762,8 +757,8 @@ static int mp_launch(const MpParams& p, int items, cudaStream_t st) {
     SM_CUDA_TRY(cudaDeviceGetAttribute(&sm_count[dev], cudaDevAttrMultiProcessorCount, dev));
     attr_set[dev] = true;
   }
-  const int smem = kMpFixed + p.ring;
-  return mx_launch(mp_product_kernel<O, GATED, PLACED>, dim3(items < sm_count[dev] ? items : sm_count[dev]), mp_threads(PLACED),
+  const int smem = kMpFixed + p.resident + p.ring;
+  return mx_launch(mp_product_kernel<O, GATED, PLACED>, dim3(items < sm_count[dev] ? items : sm_count[dev]), kMpThreads,
                    (size_t)(smem > kMpSmemMin ? smem : kMpSmemMin), st, MpParams(p));
 }
 template <class O>
@@ -817,18 +812,19 @@ extern "C" int slicemoe_mx4_product(const slicemoe_mx4_mat* mats, int n_experts,
   p.k = k;
   p.x_per_pair = x_per_pair || k == 1;
   p.k_inverse = k > 1 ? (uint32_t)((0x100000000ull + k - 1) / k) : 0;
-  p.tile = mp_tile(T);
+  // Resident where all rows fit: no launches ahead, and nothing to gather.
+  const int rows = p.x_per_pair ? pairs : T, rows16 = (rows + 15) & ~15;
+  const int64_t held = (int64_t)rows16 * mx_chunks(K) * (kMxChunk / 2) + (int64_t)mx_atoms(K) * ((rows16 + 127) / 128) * kMxAtomBytes;
+  const bool placed = pairs > kMpFew || rows16 > kMpTile || held > kMpResident;
+  p.tile = placed ? mp_tile(T) : rows16;
+  p.resident = placed ? 0 : (int)((held + 127) & ~127);
+  p.ring = kMpSmemMax - kMpFixed - p.resident;
   p.stages = kMpMaxStages;
-  p.ring = kMpSmemMax - kMpFixed;
-  if (pairs <= kMpInline) {  // steps of one size, whose places the gatherers know from their barrier
-    const int step = (int)mp_step_bytes(p.tile, (p.tile + 127) / 128);
-    if (p.stages > p.ring / step) p.stages = p.ring / step;
-    p.ring = p.stages * step;
-  }
+  if (!placed && p.stages > p.ring / (kMpABytes + kMpAScaleBytes)) p.stages = p.ring / (kMpABytes + kMpAScaleBytes);
   p.row_blocks = mx_row_blocks(N, gated);
-  const int64_t tiles = (int64_t)pairs / p.tile + (pairs < E ? pairs : E), items = tiles * p.row_blocks;
+  const int64_t tiles = placed ? (int64_t)pairs / p.tile + (pairs < E ? pairs : E) : pairs, items = tiles * p.row_blocks;
   if (items > INT32_MAX) return SLICEMOE_E_UNSUPPORTED;
-  if (pairs > kMpInline) {
+  if (placed) {
     int *rank = reinterpret_cast<int*>(ws + l.rank), *hist = reinterpret_cast<int*>(ws + l.hist), *first = reinterpret_cast<int*>(ws + l.first),
         *list = reinterpret_cast<int*>(ws + l.list);
     if (ids) {
