@@ -42,10 +42,10 @@ __host__ __device__ inline MpTiles mp_tiles(int rows, int tile) {
 // An expert has at most T rows where no token names one twice: wider tiles would only take room from the ring.
 __host__ __device__ inline int mp_tile(int T) { return T >= kMpTile ? kMpTile : (T + 15) & ~15; }
 
-// Workspace: header; ranks of the pairs among the block's of their expert, and the blocks' counts; rows, tiles and tiles' rows before each
+// Workspace: header; the pairs by expert of each block of them, and where an expert's begin there; rows, tiles and tiles' rows before each
 // expert; the pairs by expert; token rows in the operand layout.  Every part grows with each argument, so that a workspace serves smaller calls.
 struct MpLayout {
-  size_t rank, hist, first, list, scale, codes, total;
+  size_t block_list, block_first, first, list, scale, codes, total;
   int blocks;
 };
 __host__ __device__ inline MpLayout mp_layout(int T, int k, int E, int K) {
@@ -53,9 +53,9 @@ __host__ __device__ inline MpLayout mp_layout(int T, int k, int E, int K) {
   const int64_t pairs = (int64_t)T * k, tiles = (pairs / kMpTile > k ? pairs / kMpTile : k) + (pairs < E ? pairs : E) + 1;
   MpLayout l;
   l.blocks = (int)((pairs + kMpSortPairs - 1) / kMpSortPairs);
-  l.rank = 256;
-  l.hist = l.rank + up(pairs * sizeof(int));
-  l.first = l.hist + up((size_t)l.blocks * E * sizeof(int));
+  l.block_list = 256;
+  l.block_first = l.block_list + up(pairs * sizeof(int));
+  l.first = l.block_first + up((size_t)l.blocks * (E + 1) * sizeof(int));
   l.list = l.first + up((size_t)3 * (E + 1) * sizeof(int));
   l.scale = l.list + up(pairs * sizeof(int));
   l.codes = l.scale + up((size_t)tiles * 2 * mx_atoms(K) * kMxAtomBytes);
@@ -85,66 +85,71 @@ __device__ __forceinline__ int mp_scan(int v, int* s, int* total) {
 struct MpSortParams {
   const int32_t* ids;
   int pairs, E;
-  int* rank;
-  int* hist;  // [block][E]
+  int* list;   // [block][kMpSortPairs]
+  int* first;  // [block][E + 1]
   MpHeader* head;
 };
-// A pair's rank among the block's of its expert is what the counting atomic returns.  (It depends on the atomics' order; which column
-// of a tile a pair gets does not enter its result.)
+// A block's pairs by expert: a pair's rank among the block's of its expert is what the counting atomic returns.  (The order within an
+// expert depends on the atomics' order; which column of a tile a pair gets does not enter its result.)
 __global__ void __launch_bounds__(kMpSortThreads) mp_sort_kernel(const MpSortParams p) {
-  __shared__ int s_count[kMpMaxExperts];
+  __shared__ int s_first[kMpMaxExperts + 1], s_sums[32];
   mx_dep_launch();
   const int tid = threadIdx.x;
-  s_count[tid] = 0;
+  s_first[tid] = 0;
   mx_dep_wait();
   __syncthreads();
   constexpr int kEach = kMpSortPairs / kMpSortThreads;
-  const int base = blockIdx.x * kMpSortPairs + tid;
-  int e[kEach];
+  const int base = blockIdx.x * kMpSortPairs;
+  int e[kEach], rank[kEach];
   bool bad = false;
 #pragma unroll
   for (int i = 0; i < kEach; ++i) {
-    const int at = base + i * kMpSortThreads;
+    const int at = base + i * kMpSortThreads + tid;
     e[i] = at < p.pairs ? __ldcg(p.ids + at) : -1;
     bad |= at < p.pairs && (unsigned)e[i] >= (unsigned)p.E;
   }
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) {
-    const int at = base + i * kMpSortThreads;
-    if (at < p.pairs) p.rank[at] = (unsigned)e[i] < (unsigned)p.E ? atomicAdd(&s_count[e[i]], 1) : -1;
-  }
+  for (int i = 0; i < kEach; ++i) rank[i] = (unsigned)e[i] < (unsigned)p.E ? atomicAdd(&s_first[e[i]], 1) : 0;
   __syncthreads();
-  if (tid < p.E) p.hist[(size_t)blockIdx.x * p.E + tid] = s_count[tid];
+  int total;
+  const int before = mp_scan<kMpSortThreads>(s_first[tid], s_sums, &total);
+  s_first[tid] = before;
+  if (tid == 0) s_first[kMpMaxExperts] = total;
+  __syncthreads();
+  for (int i = tid; i <= p.E; i += kMpSortThreads) p.first[(size_t)blockIdx.x * (p.E + 1) + i] = s_first[i];
+#pragma unroll
+  for (int i = 0; i < kEach; ++i)
+    if ((unsigned)e[i] < (unsigned)p.E) p.list[base + s_first[e[i]] + rank[i]] = base + i * kMpSortThreads + tid;
   if (bad) atomicOr(&p.head->status, (unsigned)SLICEMOE_STATUS_BAD_EXPERT_ID);
 }
 
 struct MpPlaceParams {
-  const int32_t* ids;  // NULL: all of expert 0, in order
-  const int *rank, *hist;
+  const int *block_list, *block_first;  // NULL: all pairs are of expert 0, in order
   const uint8_t *codes, *scale;
   int *first, *list;    // first: [3][E + 1], rows, tiles and tiles' rows before an expert
   uint8_t *t_codes, *t_scale;
-  int pairs, E, blocks, chunk, tile, k, x_per_pair, K;
+  int pairs, E, blocks, tile, k, x_per_pair, K;
 };
-// Each pair's row to its place in its tile, in the layout of the tensor instruction's operand: a tile's 16-byte pieces [piece][row],
-// its scales as those of packed weights.  A block takes `chunk` pairs of one block of ranks.
+// The rows of the tiles in the layout of the tensor instruction's operand: 16-byte pieces [piece][row of the tile], scales as those of packed
+// weights.  A warp takes eight rows of a tile and every kMpPlaceSplit'th four pieces: it reads 64 bytes of a row and writes 128 that lie
+// together.  (By pairs in the order of the list, whose neighbours go to different tiles, the writes are of 16 bytes: 15 us for 8,192
+// rows of 2,048 values, 41 for 49,152 of 1,408.)
+constexpr int kMpPlaceSplit = 2;
 __global__ void __launch_bounds__(kMpPlaceThreads) mp_place_kernel(const MpPlaceParams p) {
-  __shared__ int s_first[kMpMaxExperts], s_before[kMpMaxExperts], s_count[kMpMaxExperts], s_tile[kMpMaxExperts], s_row[kMpMaxExperts], s_sums[32];
+  __shared__ int s_first[kMpMaxExperts + 1], s_tile[kMpMaxExperts], s_row[kMpMaxExperts + 1], s_sums[32];
   mx_dep_launch();
   mx_dep_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int base = blockIdx.x * p.chunk, me = base / kMpSortPairs;
   int rows = 0, tiles = 0, padded = 0;
   for (int e0 = 0; e0 < p.E; e0 += kMpPlaceThreads) {
     const int e = e0 + tid;
-    int count = 0, before = 0;
+    int count = 0;
     if (e < p.E) {
-      if (p.ids) {
+      if (p.block_list) {
 #pragma unroll 4
         for (int b = 0; b < p.blocks; ++b) {
-          const int n = __ldcg(p.hist + (size_t)b * p.E + e);
-          count += n;
-          before += b < me ? n : 0;
+          const int* f = p.block_first + (size_t)b * (p.E + 1) + e;
+          count += __ldcg(f + 1) - __ldcg(f);
         }
       } else {
         count = p.pairs;
@@ -159,42 +164,88 @@ __global__ void __launch_bounds__(kMpPlaceThreads) mp_place_kernel(const MpPlace
     const int r = padded + mp_scan<kMpPlaceThreads>(t.n * t.each, s_sums, &total);
     padded += total;
     if (e < p.E) {
-      s_first[e] = f, s_before[e] = before, s_count[e] = count, s_tile[e] = o, s_row[e] = r;
+      s_first[e] = f, s_tile[e] = o, s_row[e] = r;
       if (blockIdx.x == 0) p.first[e] = f, p.first[p.E + 1 + e] = o, p.first[2 * (p.E + 1) + e] = r;
     }
   }
+  if (tid == 0) s_first[p.E] = rows, s_row[p.E] = padded;
   if (blockIdx.x == 0 && tid == 0) p.first[p.E] = rows, p.first[2 * p.E + 1] = tiles;
   __syncthreads();
   const int chunks = mx_chunks(p.K), atoms = mx_atoms(p.K), pieces = 2 * chunks, kbytes = p.K >> 1, halves = (p.tile + 127) >> 7;
-  for (int i = warp * 8; i < p.chunk; i += kMpPlaceThreads / 32 * 8) {
-    const int pair = base + i + (lane & 7);
-    int e = -1, pos = 0;
-    if (pair < p.pairs) {
-      e = p.ids ? __ldcg(p.ids + pair) : 0;
-      if ((unsigned)e >= (unsigned)p.E) e = -1;
-      else pos = p.ids ? s_before[e] + __ldcg(p.rank + pair) : pair;
+  const int units = padded / 8 * kMpPlaceSplit;
+  for (int u = blockIdx.x * (kMpPlaceThreads / 32) + warp; u < units; u += gridDim.x * (kMpPlaceThreads / 32)) {
+    const int row8 = u / kMpPlaceSplit * 8, part = u - u / kMpPlaceSplit * kMpPlaceSplit;
+    int e = 0;  // the last expert whose first row is not above row8
+    for (int hi = p.E; hi - e > 1;) {
+      const int mid = (e + hi) >> 1;
+      if (s_row[mid] <= row8) e = mid; else hi = mid;
     }
-    if (e < 0) continue;  // no lane waits for another
-    const MpTiles t = mp_tiles(s_count[e], p.tile);
-    const int tile = pos / t.each, r = pos - tile * t.each;
+    const int count = s_first[e + 1] - s_first[e];
+    const MpTiles t = mp_tiles(count, p.tile);
+    const int in = row8 - s_row[e], tile = in / t.each, r = in - tile * t.each + (lane & 7), pos = tile * t.each + r;
+    int pair = pos < count ? pos : -1;
+    if (p.block_list) {  // the block of pairs that the row is in: a lane per block looks at how many of the expert's each has
+      int at = -1, before = 0;
+      for (int b0 = 0; b0 < p.blocks; b0 += 32) {
+        int lo = 0, n = 0;
+        if (b0 + lane < p.blocks) {
+          const int* f = p.block_first + (size_t)(b0 + lane) * (p.E + 1) + e;
+          lo = __ldcg(f);
+          n = __ldcg(f + 1) - lo;
+        }
+        int inc = n;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+          const int o = __shfl_up_sync(0xffffffffu, inc, off);
+          if (lane >= off) inc += o;
+        }
+        int idx = 0;  // blocks here that end at or before the row
+#pragma unroll
+        for (int step = 16; step > 0; step >>= 1) {
+          const int v = __shfl_sync(0xffffffffu, inc, idx + step - 1);
+          if (before + v <= pos) idx += step;
+        }
+        const int end = __shfl_sync(0xffffffffu, inc, idx), size = __shfl_sync(0xffffffffu, n, idx), start = __shfl_sync(0xffffffffu, lo, idx);
+        if (at < 0 && before + end > pos && before + end - size <= pos) at = (b0 + idx) * kMpSortPairs + start + pos - (before + end - size);
+        before += __shfl_sync(0xffffffffu, inc, 31);
+      }
+      if (pair >= 0) pair = __ldcg(p.block_list + at);
+    }
+    if (pair < 0) continue;  // no lane waits for another
     const int64_t x = p.x_per_pair ? pair : pair / p.k;
     const uint8_t* src = p.codes + x * kbytes;
     uint8_t* dst = p.t_codes + (size_t)(s_row[e] + tile * t.each) * chunks * (kMxChunk / 2) + r * 16;
-#pragma unroll 8
-    for (int q = lane >> 3; q < pieces; q += 4) {
-      const uint4 v = q * 16 < kbytes ? __ldcg(reinterpret_cast<const uint4*>(src) + q) : make_uint4(0, 0, 0, 0);
-      *reinterpret_cast<uint4*>(dst + (size_t)q * t.each * 16) = v;
-    }
+    // (loads first, then stores: left to itself the compiler cannot know that they do not overlap, and waits for each)
+    constexpr int kAhead = 8, kStep = 4 * kMpPlaceSplit;
     const uint32_t* s = reinterpret_cast<const uint32_t*>(p.scale + x * (4 * atoms));
     uint8_t* sd = p.t_scale + (size_t)(s_tile[e] + tile) * atoms * halves * kMxAtomBytes + (r >> 7) * kMxAtomBytes + (r & 31) * 16 + ((r >> 5) & 3) * 4;
-#pragma unroll 4
-    for (int j = lane >> 3; j < atoms; j += 4) {
-      const int left = (p.K >> 5) - 4 * j;
-      uint32_t w = __ldcg(s + j);
-      if (left < 4) w &= (1u << (8 * left)) - 1u;  // bytes beyond the row's end
-      *reinterpret_cast<uint32_t*>(sd + (size_t)j * halves * kMxAtomBytes) = w;
+    const int q0 = part * 4 + (lane >> 3);
+    uint32_t w[kAhead / 4];
+#pragma unroll
+    for (int i = 0; i < kAhead / 4; ++i) w[i] = q0 + i * kStep < atoms ? __ldcg(s + q0 + i * kStep) : 0u;
+    for (int b = q0; b < pieces; b += kAhead * kStep) {
+      uint4 v[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const int q = b + i * kStep;
+        v[i] = q * 16 < kbytes ? __ldcg(reinterpret_cast<const uint4*>(src) + q) : make_uint4(0, 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const int q = b + i * kStep;
+        if (q < pieces) *reinterpret_cast<uint4*>(dst + (size_t)q * t.each * 16) = v[i];
+      }
     }
-    if (lane < 8) p.list[s_first[e] + pos] = pair;
+    for (int b = q0; b < atoms; b += kAhead / 4 * kStep) {
+#pragma unroll
+      for (int i = 0; i < kAhead / 4; ++i) {
+        const int j = b + i * kStep, left = (p.K >> 5) - 4 * j;
+        if (b != q0) w[i] = j < atoms ? __ldcg(s + j) : 0u;
+        if (left < 4) w[i] &= (1u << (8 * max(left, 0))) - 1u;  // bytes beyond the row's end
+        if (j < atoms) *reinterpret_cast<uint32_t*>(sd + (size_t)j * halves * kMxAtomBytes) = w[i];
+      }
+    }
+    if (part == 0 && lane < 8) p.list[s_first[e] + pos] = pair;
   }
 }
 
@@ -825,16 +876,16 @@ extern "C" int slicemoe_mx4_product(const slicemoe_mx4_mat* mats, int n_experts,
   const int64_t tiles = placed ? (int64_t)pairs / p.tile + (pairs < E ? pairs : E) : pairs, items = tiles * p.row_blocks;
   if (items > INT32_MAX) return SLICEMOE_E_UNSUPPORTED;
   if (placed) {
-    int *rank = reinterpret_cast<int*>(ws + l.rank), *hist = reinterpret_cast<int*>(ws + l.hist), *first = reinterpret_cast<int*>(ws + l.first),
-        *list = reinterpret_cast<int*>(ws + l.list);
+    int *block_list = reinterpret_cast<int*>(ws + l.block_list), *block_first = reinterpret_cast<int*>(ws + l.block_first),
+        *first = reinterpret_cast<int*>(ws + l.first), *list = reinterpret_cast<int*>(ws + l.list);
     if (ids) {
-      const int rc = mx_launch(mp_sort_kernel, dim3(l.blocks), kMpSortThreads, 0, st, MpSortParams{ids, pairs, E, rank, hist, p.head});
+      const int rc = mx_launch(mp_sort_kernel, dim3(l.blocks), kMpSortThreads, 0, st, MpSortParams{ids, pairs, E, block_list, block_first, p.head});
       if (rc != SLICEMOE_OK) return rc;
     }
-    int chunk = 64;  // pairs of a block: more where there are blocks enough to fill the device
-    while (chunk < kMpSortPairs && pairs / chunk > 1184) chunk *= 2;
-    const MpPlaceParams pp = {ids, rank, hist, codes, scale, first, list, ws + l.codes, ws + l.scale, pairs, E, l.blocks, chunk, p.tile, k, x_per_pair, K};
-    const int rc = mx_launch(mp_place_kernel, dim3((pairs + chunk - 1) / chunk), kMpPlaceThreads, 0, st, MpPlaceParams(pp));
+    const MpPlaceParams pp = {ids ? block_list : nullptr, block_first, codes, scale, first, list, ws + l.codes, ws + l.scale, pairs, E, l.blocks,
+                              p.tile, k, x_per_pair, K};
+    const int64_t units = ((int64_t)pairs / 8 + 2 * tiles) * kMpPlaceSplit, blocks = (units + kMpPlaceThreads / 32 - 1) / (kMpPlaceThreads / 32);
+    const int rc = mx_launch(mp_place_kernel, dim3((unsigned)(blocks < 148 * 8 ? blocks : 148 * 8)), kMpPlaceThreads, 0, st, MpPlaceParams(pp));
     if (rc != SLICEMOE_OK) return rc;
     p.first = first;
     p.list = list;
