@@ -42,10 +42,19 @@ __host__ __device__ inline MpTiles mp_tiles(int rows, int tile) {
 // An expert has at most T rows where no token names one twice: wider tiles would only take room from the ring.
 __host__ __device__ inline int mp_tile(int T) { return T >= kMpTile ? kMpTile : (T + 15) & ~15; }
 
-// Workspace: header; the pairs by expert of each block of them, and where an expert's begin there; rows, tiles and tiles' rows before each
+// Token rows lie as the tensor instruction takes an operand: by steps of 256 values, in a step a row's 128 bytes after the other, their eight
+// pieces of 16 bytes swapped about by the row (piece c at c ^ (row % 8): the 128-byte swizzle).  Eight rows begin at a multiple of 1024.
+constexpr int kMpStepChunks = 4;  // chunks of 64 values a step
+constexpr int kMpRowBytes = kMpStepChunks * kMxChunk / 2;
+__host__ __device__ inline int mp_steps(int K) { return (mx_chunks(K) + kMpStepChunks - 1) / kMpStepChunks; }
+__device__ __forceinline__ uint32_t mp_piece(uint32_t rows, uint32_t row, uint32_t piece) {  // where a piece of 16 bytes lies in a tile
+  return (piece >> 3) * rows * kMpRowBytes + row * kMpRowBytes + ((piece ^ row) & 7) * 16;
+}
+
+// Workspace: header; ranks of the pairs among the block's of their expert, and the blocks' counts; rows, tiles and tiles' rows before each
 // expert; the pairs by expert; token rows in the operand layout.  Every part grows with each argument, so that a workspace serves smaller calls.
 struct MpLayout {
-  size_t block_list, block_first, first, list, scale, codes, total;
+  size_t rank, hist, first, list, scale, codes, total;
   int blocks;
 };
 __host__ __device__ inline MpLayout mp_layout(int T, int k, int E, int K) {
@@ -53,13 +62,13 @@ __host__ __device__ inline MpLayout mp_layout(int T, int k, int E, int K) {
   const int64_t pairs = (int64_t)T * k, tiles = (pairs / kMpTile > k ? pairs / kMpTile : k) + (pairs < E ? pairs : E) + 1;
   MpLayout l;
   l.blocks = (int)((pairs + kMpSortPairs - 1) / kMpSortPairs);
-  l.block_list = 256;
-  l.block_first = l.block_list + up(pairs * sizeof(int));
-  l.first = l.block_first + up((size_t)l.blocks * (E + 1) * sizeof(int));
+  l.rank = 256;
+  l.hist = l.rank + up(pairs * sizeof(int));
+  l.first = l.hist + up((size_t)l.blocks * E * sizeof(int));
   l.list = l.first + up((size_t)3 * (E + 1) * sizeof(int));
   l.scale = l.list + up(pairs * sizeof(int));
   l.codes = l.scale + up((size_t)tiles * 2 * mx_atoms(K) * kMxAtomBytes);
-  l.total = l.codes + up((size_t)(pairs + 16 * tiles) * mx_chunks(K) * (kMxChunk / 2));
+  l.total = l.codes + up((size_t)(pairs + 16 * tiles) * mp_steps(K) * kMpRowBytes);
   return l;
 }
 
@@ -85,71 +94,69 @@ __device__ __forceinline__ int mp_scan(int v, int* s, int* total) {
 struct MpSortParams {
   const int32_t* ids;
   int pairs, E;
-  int* list;   // [block][kMpSortPairs]
-  int* first;  // [block][E + 1]
+  int* rank;
+  int* hist;  // [block][E]
   MpHeader* head;
 };
-// A block's pairs by expert: a pair's rank among the block's of its expert is what the counting atomic returns.  (The order within an
-// expert depends on the atomics' order; which column of a tile a pair gets does not enter its result.)
+// A pair's rank among the block's of its expert is what the counting atomic returns.  (It depends on the atomics' order; which column
+// of a tile a pair gets does not enter its result.)
 __global__ void __launch_bounds__(kMpSortThreads) mp_sort_kernel(const MpSortParams p) {
-  __shared__ int s_first[kMpMaxExperts + 1], s_sums[32];
+  __shared__ int s_count[kMpMaxExperts];
   mx_dep_launch();
   const int tid = threadIdx.x;
-  s_first[tid] = 0;
+  s_count[tid] = 0;
   mx_dep_wait();
   __syncthreads();
   constexpr int kEach = kMpSortPairs / kMpSortThreads;
-  const int base = blockIdx.x * kMpSortPairs;
-  int e[kEach], rank[kEach];
+  const int base = blockIdx.x * kMpSortPairs + tid;
+  int e[kEach];
   bool bad = false;
 #pragma unroll
   for (int i = 0; i < kEach; ++i) {
-    const int at = base + i * kMpSortThreads + tid;
+    const int at = base + i * kMpSortThreads;
     e[i] = at < p.pairs ? __ldcg(p.ids + at) : -1;
     bad |= at < p.pairs && (unsigned)e[i] >= (unsigned)p.E;
   }
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) rank[i] = (unsigned)e[i] < (unsigned)p.E ? atomicAdd(&s_first[e[i]], 1) : 0;
+  for (int i = 0; i < kEach; ++i) {
+    const int at = base + i * kMpSortThreads;
+    if (at < p.pairs) p.rank[at] = (unsigned)e[i] < (unsigned)p.E ? atomicAdd(&s_count[e[i]], 1) : -1;
+  }
   __syncthreads();
-  int total;
-  const int before = mp_scan<kMpSortThreads>(s_first[tid], s_sums, &total);
-  s_first[tid] = before;
-  if (tid == 0) s_first[kMpMaxExperts] = total;
-  __syncthreads();
-  for (int i = tid; i <= p.E; i += kMpSortThreads) p.first[(size_t)blockIdx.x * (p.E + 1) + i] = s_first[i];
-#pragma unroll
-  for (int i = 0; i < kEach; ++i)
-    if ((unsigned)e[i] < (unsigned)p.E) p.list[base + s_first[e[i]] + rank[i]] = base + i * kMpSortThreads + tid;
+  if (tid < p.E) p.hist[(size_t)blockIdx.x * p.E + tid] = s_count[tid];
   if (bad) atomicOr(&p.head->status, (unsigned)SLICEMOE_STATUS_BAD_EXPERT_ID);
 }
 
 struct MpPlaceParams {
-  const int *block_list, *block_first;  // NULL: all pairs are of expert 0, in order
+  const int32_t* ids;  // NULL: all of expert 0, in order
+  const int *rank, *hist;
   const uint8_t *codes, *scale;
   int *first, *list;    // first: [3][E + 1], rows, tiles and tiles' rows before an expert
   uint8_t *t_codes, *t_scale;
-  int pairs, E, blocks, tile, k, x_per_pair, K;
+  int pairs, E, blocks, chunk, tile, k, x_per_pair, K;
 };
-// The rows of the tiles in the layout of the tensor instruction's operand: 16-byte pieces [piece][row of the tile], scales as those of packed
-// weights.  A warp takes eight rows of a tile and every kMpPlaceSplit'th four pieces: it reads 64 bytes of a row and writes 128 that lie
-// together.  (By pairs in the order of the list, whose neighbours go to different tiles, the writes are of 16 bytes: 15 us for 8,192
-// rows of 2,048 values, 41 for 49,152 of 1,408.)
-constexpr int kMpPlaceSplit = 2;
+// Each pair's row to its place in its tile; scales as those of packed weights.  A block takes `chunk` pairs of one block of ranks, a warp
+// four of them at a time: a row is read in runs of 512 bytes and written in runs of 128, which is what the swizzled operand layout
+// keeps together.  (Without the swizzle a row's pieces of 16 bytes lie apart: 9 us for 8,192 rows of 2,048 values and 28 for 49,152 of
+// 1,408, in whichever order the rows are taken.)
+constexpr int kMpPlaceRows = 4;
 __global__ void __launch_bounds__(kMpPlaceThreads) mp_place_kernel(const MpPlaceParams p) {
-  __shared__ int s_first[kMpMaxExperts + 1], s_tile[kMpMaxExperts], s_row[kMpMaxExperts + 1], s_sums[32];
+  __shared__ int s_first[kMpMaxExperts], s_before[kMpMaxExperts], s_count[kMpMaxExperts], s_tile[kMpMaxExperts], s_row[kMpMaxExperts], s_sums[32];
   mx_dep_launch();
   mx_dep_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int base = blockIdx.x * p.chunk, me = base / kMpSortPairs;
   int rows = 0, tiles = 0, padded = 0;
   for (int e0 = 0; e0 < p.E; e0 += kMpPlaceThreads) {
     const int e = e0 + tid;
-    int count = 0;
+    int count = 0, before = 0;
     if (e < p.E) {
-      if (p.block_list) {
-#pragma unroll 4
+      if (p.ids) {
+#pragma unroll 8
         for (int b = 0; b < p.blocks; ++b) {
-          const int* f = p.block_first + (size_t)b * (p.E + 1) + e;
-          count += __ldcg(f + 1) - __ldcg(f);
+          const int n = __ldcg(p.hist + (size_t)b * p.E + e);
+          count += n;
+          before += b < me ? n : 0;
         }
       } else {
         count = p.pairs;
@@ -164,93 +171,77 @@ __global__ void __launch_bounds__(kMpPlaceThreads) mp_place_kernel(const MpPlace
     const int r = padded + mp_scan<kMpPlaceThreads>(t.n * t.each, s_sums, &total);
     padded += total;
     if (e < p.E) {
-      s_first[e] = f, s_tile[e] = o, s_row[e] = r;
+      s_first[e] = f, s_before[e] = before, s_count[e] = count, s_tile[e] = o, s_row[e] = r;
       if (blockIdx.x == 0) p.first[e] = f, p.first[p.E + 1 + e] = o, p.first[2 * (p.E + 1) + e] = r;
     }
   }
-  if (tid == 0) s_first[p.E] = rows, s_row[p.E] = padded;
   if (blockIdx.x == 0 && tid == 0) p.first[p.E] = rows, p.first[2 * p.E + 1] = tiles;
   __syncthreads();
-  const int chunks = mx_chunks(p.K), atoms = mx_atoms(p.K), pieces = 2 * chunks, kbytes = p.K >> 1, halves = (p.tile + 127) >> 7;
-  const int units = padded / 8 * kMpPlaceSplit;
-  for (int u = blockIdx.x * (kMpPlaceThreads / 32) + warp; u < units; u += gridDim.x * (kMpPlaceThreads / 32)) {
-    const int row8 = u / kMpPlaceSplit * 8, part = u - u / kMpPlaceSplit * kMpPlaceSplit;
-    int e = 0;  // the last expert whose first row is not above row8
-    for (int hi = p.E; hi - e > 1;) {
-      const int mid = (e + hi) >> 1;
-      if (s_row[mid] <= row8) e = mid; else hi = mid;
+  const int atoms = mx_atoms(p.K), pieces = 2 * mx_chunks(p.K), kbytes = p.K >> 1, halves = (p.tile + 127) >> 7, steps = mp_steps(p.K);
+  for (int i = warp * kMpPlaceRows; i < p.chunk; i += kMpPlaceThreads / 32 * kMpPlaceRows) {
+    // lane l < 4 works out where pair i + l goes
+    const int pair = base + i + lane;
+    int64_t x = -1;
+    size_t code_at = 0, scale_at = 0;
+    int each = 0, row = 0;
+    if (lane < kMpPlaceRows && pair < p.pairs) {
+      const int e = p.ids ? __ldcg(p.ids + pair) : 0;
+      if ((unsigned)e < (unsigned)p.E) {
+        const int pos = p.ids ? s_before[e] + __ldcg(p.rank + pair) : pair, count = s_count[e];
+        const MpTiles t = count <= p.tile ? MpTiles{1, (count + 15) & ~15} : mp_tiles(count, p.tile);
+        const int tile = t.n == 1 ? 0 : pos / t.each;
+        row = pos - tile * t.each;
+        each = t.each;
+        x = p.x_per_pair ? pair : pair / p.k;
+        code_at = (size_t)(s_row[e] + tile * t.each) * steps * kMpRowBytes;
+        scale_at = (size_t)(s_tile[e] + tile) * atoms * halves * kMxAtomBytes + (row >> 7) * kMxAtomBytes + (row & 31) * 16 + ((row >> 5) & 3) * 4;
+        p.list[s_first[e] + pos] = pair;
+      }
     }
-    const int count = s_first[e + 1] - s_first[e];
-    const MpTiles t = mp_tiles(count, p.tile);
-    const int in = row8 - s_row[e], tile = in / t.each, r = in - tile * t.each + (lane & 7), pos = tile * t.each + r;
-    int pair = pos < count ? pos : -1;
-    if (p.block_list) {  // the block of pairs that the row is in: a lane per block looks at how many of the expert's each has
-      int at = -1, before = 0;
-      for (int b0 = 0; b0 < p.blocks; b0 += 32) {
-        int lo = 0, n = 0;
-        if (b0 + lane < p.blocks) {
-          const int* f = p.block_first + (size_t)(b0 + lane) * (p.E + 1) + e;
-          lo = __ldcg(f);
-          n = __ldcg(f + 1) - lo;
+    int64_t xs[kMpPlaceRows];
+    size_t cs[kMpPlaceRows], ss[kMpPlaceRows];
+    int es[kMpPlaceRows], rs[kMpPlaceRows];
+#pragma unroll
+    for (int l = 0; l < kMpPlaceRows; ++l) {
+      xs[l] = __shfl_sync(0xffffffffu, x, l);
+      cs[l] = __shfl_sync(0xffffffffu, code_at, l);
+      ss[l] = __shfl_sync(0xffffffffu, scale_at, l);
+      es[l] = __shfl_sync(0xffffffffu, each, l);
+      rs[l] = __shfl_sync(0xffffffffu, row, l);
+    }
+    // loads first, then stores: left to itself the compiler cannot know that they do not overlap, and waits for each
+    for (int q0 = 0; q0 < pieces; q0 += 64) {
+      uint4 v[kMpPlaceRows][2];
+#pragma unroll
+      for (int l = 0; l < kMpPlaceRows; ++l)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int q = q0 + 32 * h + lane;
+          v[l][h] = xs[l] >= 0 && q * 16 < kbytes ? __ldcg(reinterpret_cast<const uint4*>(p.codes + xs[l] * kbytes) + q) : make_uint4(0, 0, 0, 0);
         }
-        int inc = n;
 #pragma unroll
-        for (int off = 1; off < 32; off <<= 1) {
-          const int o = __shfl_up_sync(0xffffffffu, inc, off);
-          if (lane >= off) inc += o;
+      for (int l = 0; l < kMpPlaceRows; ++l)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int q = q0 + 32 * h + lane;
+          if (xs[l] >= 0 && q < pieces) *reinterpret_cast<uint4*>(p.t_codes + cs[l] + mp_piece(es[l], rs[l], q)) = v[l][h];
         }
-        int idx = 0;  // blocks here that end at or before the row
-#pragma unroll
-        for (int step = 16; step > 0; step >>= 1) {
-          const int v = __shfl_sync(0xffffffffu, inc, idx + step - 1);
-          if (before + v <= pos) idx += step;
-        }
-        const int end = __shfl_sync(0xffffffffu, inc, idx), size = __shfl_sync(0xffffffffu, n, idx), start = __shfl_sync(0xffffffffu, lo, idx);
-        if (at < 0 && before + end > pos && before + end - size <= pos) at = (b0 + idx) * kMpSortPairs + start + pos - (before + end - size);
-        before += __shfl_sync(0xffffffffu, inc, 31);
-      }
-      if (pair >= 0) pair = __ldcg(p.block_list + at);
     }
-    if (pair < 0) continue;  // no lane waits for another
-    const int64_t x = p.x_per_pair ? pair : pair / p.k;
-    const uint8_t* src = p.codes + x * kbytes;
-    uint8_t* dst = p.t_codes + (size_t)(s_row[e] + tile * t.each) * chunks * (kMxChunk / 2) + r * 16;
-    // (loads first, then stores: left to itself the compiler cannot know that they do not overlap, and waits for each)
-    constexpr int kAhead = 8, kStep = 4 * kMpPlaceSplit;
-    const uint32_t* s = reinterpret_cast<const uint32_t*>(p.scale + x * (4 * atoms));
-    uint8_t* sd = p.t_scale + (size_t)(s_tile[e] + tile) * atoms * halves * kMxAtomBytes + (r >> 7) * kMxAtomBytes + (r & 31) * 16 + ((r >> 5) & 3) * 4;
-    const int q0 = part * 4 + (lane >> 3);
-    uint32_t w[kAhead / 4];
+    for (int j = lane; j < atoms; j += 32) {
+      const int left = (p.K >> 5) - 4 * j;
+      uint32_t w[kMpPlaceRows];
 #pragma unroll
-    for (int i = 0; i < kAhead / 4; ++i) w[i] = q0 + i * kStep < atoms ? __ldcg(s + q0 + i * kStep) : 0u;
-    for (int b = q0; b < pieces; b += kAhead * kStep) {
-      uint4 v[kAhead];
+      for (int l = 0; l < kMpPlaceRows; ++l) w[l] = xs[l] >= 0 ? __ldcg(reinterpret_cast<const uint32_t*>(p.scale + xs[l] * (4 * atoms)) + j) : 0u;
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        const int q = b + i * kStep;
-        v[i] = q * 16 < kbytes ? __ldcg(reinterpret_cast<const uint4*>(src) + q) : make_uint4(0, 0, 0, 0);
-      }
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        const int q = b + i * kStep;
-        if (q < pieces) *reinterpret_cast<uint4*>(dst + (size_t)q * t.each * 16) = v[i];
+      for (int l = 0; l < kMpPlaceRows; ++l) {
+        if (left < 4) w[l] &= (1u << (8 * left)) - 1u;  // bytes beyond the row's end
+        if (xs[l] >= 0) *reinterpret_cast<uint32_t*>(p.t_scale + ss[l] + (size_t)j * halves * kMxAtomBytes) = w[l];
       }
     }
-    for (int b = q0; b < atoms; b += kAhead / 4 * kStep) {
-#pragma unroll
-      for (int i = 0; i < kAhead / 4; ++i) {
-        const int j = b + i * kStep, left = (p.K >> 5) - 4 * j;
-        if (b != q0) w[i] = j < atoms ? __ldcg(s + j) : 0u;
-        if (left < 4) w[i] &= (1u << (8 * max(left, 0))) - 1u;  // bytes beyond the row's end
-        if (j < atoms) *reinterpret_cast<uint32_t*>(sd + (size_t)j * halves * kMxAtomBytes) = w[i];
-      }
-    }
-    if (part == 0 && lane < 8) p.list[s_first[e] + pos] = pair;
   }
 }
 
 // ---- the product ----------------------------------------------------------------------------------------------------
-constexpr int kMpStepChunks = 4;             // chunks of 64 values a step
 constexpr int kMpWeightWarp = 0, kMpMmaWarp = 1, kMpPlanWarp = 2, kMpFirstDrain = 4, kMpDrainWarps = 8;  // warp 3 helps to lay out resident rows
 constexpr int kMpThreads = 32 * (kMpFirstDrain + kMpDrainWarps);
 constexpr int kMpTable = 128;                // table entries that a CTA keeps in shared memory
@@ -287,13 +278,13 @@ struct __align__(16) MpSmem {
 };
 static_assert(offsetof(MpSmem, pair) % 16 == 0 && kMpTile % 4 == 0 && offsetof(MpSmem, mats) % 8 == 0, "alignment");
 static_assert(offsetof(MpSmem, limit) == offsetof(MpSmem, dead) + 8, "wait_limit()");
-constexpr int kMpFixed = (int)((sizeof(MpSmem) + 127) / 128 * 128);
+constexpr int kMpFixed = (int)((sizeof(MpSmem) + 1023) / 1024 * 1024);
 constexpr int kMpSmemMax = 227 * 1024, kMpSmemMin = 116 * 1024;  // one CTA to an SM: each takes all of tensor memory
 
 // A step in the ring: weights, their scales, token rows, their scales.  Steps lie one behind the other, each as long as its item's
 // tile needs, and start again at 0 where the next does not fit: who fills and who reads work out the same places.
 __host__ __device__ constexpr uint32_t mp_step_bytes(int rows, int halves) {
-  return kMpABytes + kMpAScaleBytes + rows * (kMpStepChunks * kMxChunk / 2) + halves * kMpAScaleBytes;
+  return kMpABytes + kMpAScaleBytes + rows * kMpRowBytes + halves * kMpAScaleBytes;
 }
 __device__ __forceinline__ uint32_t mp_next_place(uint32_t& head, uint32_t bytes, uint32_t ring) {
   const uint32_t at = head + bytes <= ring ? head : 0;
@@ -318,10 +309,12 @@ struct MpParams {
   int row_blocks;
 };
 
-// Operand descriptors without swizzle: 8 rows x 16 bytes one after the other, 128 bytes on to the next eight rows (operands and scales
+// Operand descriptors without swizzle: 8 rows x 16 bytes one after the other, 128 bytes on to the next eight rows (weights and all scales
 // alike), `lead` bytes to the next 16 bytes of a row.  The upper half is the same for all.
-constexpr uint32_t kMpDescHigh = (128 >> 4) | 1u << 14;
+constexpr uint32_t kMpDescHigh = (128 >> 4) | 1u << 14, kMpDescSwizzled = (1024 >> 4) | 1u << 14 | 2u << 29;
 __device__ __forceinline__ uint64_t mp_desc(uint32_t low) { return (uint64_t)kMpDescHigh << 32 | low; }
+// Of token rows: 128-byte swizzle, 1024 bytes to the next eight rows.
+__device__ __forceinline__ uint64_t mp_desc_rows(uint32_t low) { return (uint64_t)kMpDescSwizzled << 32 | low; }
 // E2M1 x E2M1, E8M0 scales, M 128, N tokens.  Bits 29 and 4: which pair of the four scale bytes, see mp_mma.
 __device__ __forceinline__ uint32_t mp_idesc(int n) {
   return (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | (1u << 23) | ((uint32_t)(kMxRows >> 4) << 24);
@@ -382,7 +375,7 @@ __device__ __forceinline__ uint32_t mp_pack2(float a, float b) {
 // nothing has to be gathered.
 template <class O, bool GATED, bool PLACED>
 __global__ void __launch_bounds__(kMpThreads, 1) mp_product_kernel(const MpParams p) {
-  extern __shared__ __align__(128) uint8_t mp_smem[];
+  extern __shared__ __align__(1024) uint8_t mp_smem[];
   MpSmem* s = reinterpret_cast<MpSmem*>(mp_smem);
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int chunks = mx_chunks(p.K), atoms = mx_atoms(p.K), steps = (chunks + kMpStepChunks - 1) / kMpStepChunks;
@@ -525,7 +518,7 @@ __global__ void __launch_bounds__(kMpThreads, 1) mp_product_kernel(const MpParam
         const int t = local - rb * tt.n, r0 = t * tt.each, n = min(tt.each, count - r0), n16 = (n + 15) & ~15;
         for (int i = lane; i < n16; i += 32) s->pair[slot][i] = i < n ? __ldcg(p.list + first + r0 + i) : -1;
         if (lane == 0) {
-          item->t_codes = p.t_codes + (size_t)(s->padded[e] + r0) * chunks * (kMxChunk / 2);
+          item->t_codes = p.t_codes + (size_t)(s->padded[e] + r0) * steps * kMpRowBytes;
           item->t_scale = p.t_scale + (size_t)(e_tile + t) * atoms * halves * kMxAtomBytes;
           item->n = n16;
           item->rows = tt.each;
@@ -571,7 +564,7 @@ __global__ void __launch_bounds__(kMpThreads, 1) mp_product_kernel(const MpParam
       while (ok && (ok = mbar_wait(smem_u32(&s->item_full[slot]), turn, &s->dead, status))) {
         const MpItem item = s->item[slot];
         if (item.n < 0) break;
-        const uint32_t bytes = PLACED ? mp_step_bytes(item.rows, halves) : kMpABytes + kMpAScaleBytes, t_step = item.rows * (kMpStepChunks * kMxChunk / 2);
+        const uint32_t bytes = PLACED ? mp_step_bytes(item.rows, halves) : kMpABytes + kMpAScaleBytes, t_step = item.rows * kMpRowBytes;
         for (int i = 0; i < steps; ++i) {
           uint32_t at;
           for (;;) {
@@ -592,7 +585,7 @@ __global__ void __launch_bounds__(kMpThreads, 1) mp_product_kernel(const MpParam
           if (bring) {
             const int c = min(kMpStepChunks, chunks - i * kMpStepChunks), a = (c + 1) >> 1;
             const uint32_t dst = ring + at, bar = smem_u32(&s->full[st]);
-            const uint32_t t_bytes = PLACED ? c * item.rows * (kMxChunk / 2) : 0, ts_bytes = PLACED ? a * halves * kMxAtomBytes : 0;
+            const uint32_t t_bytes = PLACED ? t_step : 0, ts_bytes = PLACED ? a * halves * kMxAtomBytes : 0;
             mbar_arrive_expect_tx(bar, c * kMxChunkBytes + a * kMxAtomBytes + t_bytes + ts_bytes);
             mp_bulk(dst, item.codes + (size_t)i * kMpABytes, c * kMxChunkBytes, bar);
             mp_bulk(dst + kMpABytes, item.scale + (size_t)i * kMpAScaleBytes, a * kMxAtomBytes, bar);
@@ -629,7 +622,7 @@ __global__ void __launch_bounds__(kMpThreads, 1) mp_product_kernel(const MpParam
         if (n < 0) break;
         const uint32_t idesc = mp_idesc(n), d = tmem + acc * kMpTile;
         const bool wide = n > 128;
-        const uint32_t b_bytes = rows * (kMpStepChunks * kMxChunk / 2), bytes = PLACED ? mp_step_bytes(rows, halves) : kMpABytes + kMpAScaleBytes;
+        const uint32_t b_bytes = rows * kMpRowBytes, bytes = PLACED ? mp_step_bytes(rows, halves) : kMpABytes + kMpAScaleBytes;
         if (!(ok = mbar_wait(smem_u32(&s->acc_free[acc]), acc_ph ^ 1u, &s->dead, status))) break;
         mp_fence_after();
         for (int i = 0; i < steps; ++i) {
@@ -637,8 +630,8 @@ __global__ void __launch_bounds__(kMpThreads, 1) mp_product_kernel(const MpParam
           mp_fence_after();
           const int c = chunks - i * kMpStepChunks;  // chunks of the step, if below four
           const uint32_t at = ring + mp_next_place(head, bytes, p.ring), b_at = PLACED ? at + kMpABytes + kMpAScaleBytes : rows_at + i * b_bytes;
-          const uint32_t la = (at >> 4) + ((kMxRows * 16 >> 4) << 16), lb = (b_at >> 4) + ((uint32_t)rows << 16);
-          const uint32_t s_at = PLACED ? b_at + b_bytes : rows_at + chunks * rows * (kMxChunk / 2) + i * halves * kMpAScaleBytes;
+          const uint32_t la = (at >> 4) + ((kMxRows * 16 >> 4) << 16), lb = (b_at >> 4) + (1u << 16);
+          const uint32_t s_at = PLACED ? b_at + b_bytes : rows_at + steps * b_bytes + i * halves * kMpAScaleBytes;
           const uint32_t lsa = (at + kMpABytes) >> 4, lsb = s_at >> 4, next = halves * (kMxAtomBytes >> 4);
           const uint32_t sa = tmem + kMpScaleCol + flip * kMpScaleCols, sb = sa + 8;
           mp_copy_scales(sa, mp_desc(lsa));
@@ -653,7 +646,7 @@ __global__ void __launch_bounds__(kMpThreads, 1) mp_product_kernel(const MpParam
           for (int j = 0; j < kMpStepChunks; ++j)
             if (j < c) {
               constexpr uint32_t kHigh = 2u << 29 | 2u << 4;  // the upper two of the four scale bytes
-              mp_mma(d, mp_desc(la + j * (kMxChunkBytes >> 4)), mp_desc(lb + j * 2 * rows), j & 1 ? idesc | kHigh : idesc, sa + 4 * (j >> 1),
+              mp_mma(d, mp_desc(la + j * (kMxChunkBytes >> 4)), mp_desc_rows(lb + j * (kMxChunk / 2 >> 4)), j & 1 ? idesc | kHigh : idesc, sa + 4 * (j >> 1),
                      sb + 8 * (j >> 1), (uint32_t)(i | j));
             }
           mp_commit(smem_u32(&s->free_[st]));
@@ -675,16 +668,16 @@ __global__ void __launch_bounds__(kMpThreads, 1) mp_product_kernel(const MpParam
     __syncwarp();
   } else {
     if constexpr (!PLACED) {
-      // ---- all rows of the call into the operand layout, eight rows x four pieces of 16 bytes at a time ----
+      // ---- all rows of the call into the operand layout, 512 bytes of a row at a time ----
       mx_dep_wait();
-      const int rows = p.x_per_pair ? pairs : p.T, kbytes = p.K >> 1, pieces = 2 * chunks, scales = rows_at + chunks * p.tile * (kMxChunk / 2);
-      const int eights = (rows + 7) >> 3, quads = (pieces + 3) >> 2;
-      for (int i = warp - 3; i < eights * quads; i += kMpDrainWarps + 1) {
-        const int quad = i / eights, r = (i - quad * eights) * 8 + (lane & 7), q = quad * 4 + (lane >> 3);
-        if (r < rows && q < pieces) {  // beyond the row's end zeros; all of a lane's copies are under way at once
+      const int rows = p.x_per_pair ? pairs : p.T, kbytes = p.K >> 1, pieces = 2 * chunks, scales = rows_at + steps * p.tile * kMpRowBytes;
+      const int runs = (pieces + 31) >> 5;
+      for (int i = warp - 3; i < rows * runs; i += kMpDrainWarps + 1) {
+        const int r = i / runs, q = (i - r * runs) * 32 + lane;
+        if (q < pieces) {  // beyond the row's end zeros; all of a lane's copies are under way at once
           const uint8_t* src = p.codes + (size_t)r * kbytes;
           const bool in = q * 16 < kbytes;
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(rows_at + (q * p.tile + r) * 16), "l"(in ? src + q * 16 : src),
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(rows_at + mp_piece(p.tile, r, q)), "l"(in ? src + q * 16 : src),
                        "r"(in ? 16u : 0u)
                        : "memory");
         }
@@ -865,10 +858,10 @@ extern "C" int slicemoe_mx4_product(const slicemoe_mx4_mat* mats, int n_experts,
   p.k_inverse = k > 1 ? (uint32_t)((0x100000000ull + k - 1) / k) : 0;
   // Resident where all rows fit: no launches ahead, and nothing to gather.
   const int rows = p.x_per_pair ? pairs : T, rows16 = (rows + 15) & ~15;
-  const int64_t held = (int64_t)rows16 * mx_chunks(K) * (kMxChunk / 2) + (int64_t)mx_atoms(K) * ((rows16 + 127) / 128) * kMxAtomBytes;
+  const int64_t held = (int64_t)rows16 * mp_steps(K) * kMpRowBytes + (int64_t)mx_atoms(K) * ((rows16 + 127) / 128) * kMxAtomBytes;
   const bool placed = pairs > kMpFew || rows16 > kMpTile || held > kMpResident;
   p.tile = placed ? mp_tile(T) : rows16;
-  p.resident = placed ? 0 : (int)((held + 127) & ~127);
+  p.resident = placed ? 0 : (int)((held + 1023) & ~1023);
   p.ring = kMpSmemMax - kMpFixed - p.resident;
   p.stages = kMpMaxStages;
   if (!placed && p.stages > p.ring / (kMpABytes + kMpAScaleBytes)) p.stages = p.ring / (kMpABytes + kMpAScaleBytes);
@@ -876,16 +869,16 @@ extern "C" int slicemoe_mx4_product(const slicemoe_mx4_mat* mats, int n_experts,
   const int64_t tiles = placed ? (int64_t)pairs / p.tile + (pairs < E ? pairs : E) : pairs, items = tiles * p.row_blocks;
   if (items > INT32_MAX) return SLICEMOE_E_UNSUPPORTED;
   if (placed) {
-    int *block_list = reinterpret_cast<int*>(ws + l.block_list), *block_first = reinterpret_cast<int*>(ws + l.block_first),
-        *first = reinterpret_cast<int*>(ws + l.first), *list = reinterpret_cast<int*>(ws + l.list);
+    int *rank = reinterpret_cast<int*>(ws + l.rank), *hist = reinterpret_cast<int*>(ws + l.hist), *first = reinterpret_cast<int*>(ws + l.first),
+        *list = reinterpret_cast<int*>(ws + l.list);
     if (ids) {
-      const int rc = mx_launch(mp_sort_kernel, dim3(l.blocks), kMpSortThreads, 0, st, MpSortParams{ids, pairs, E, block_list, block_first, p.head});
+      const int rc = mx_launch(mp_sort_kernel, dim3(l.blocks), kMpSortThreads, 0, st, MpSortParams{ids, pairs, E, rank, hist, p.head});
       if (rc != SLICEMOE_OK) return rc;
     }
-    const MpPlaceParams pp = {ids ? block_list : nullptr, block_first, codes, scale, first, list, ws + l.codes, ws + l.scale, pairs, E, l.blocks,
-                              p.tile, k, x_per_pair, K};
-    const int64_t units = ((int64_t)pairs / 8 + 2 * tiles) * kMpPlaceSplit, blocks = (units + kMpPlaceThreads / 32 - 1) / (kMpPlaceThreads / 32);
-    const int rc = mx_launch(mp_place_kernel, dim3((unsigned)(blocks < 148 * 8 ? blocks : 148 * 8)), kMpPlaceThreads, 0, st, MpPlaceParams(pp));
+    int chunk = kMpPlaceThreads / 32 * kMpPlaceRows;  // pairs of a block: more where there are blocks enough to fill the device
+    while (chunk < kMpSortPairs && pairs / chunk > 148 * 4) chunk *= 2;
+    const MpPlaceParams pp = {ids, rank, hist, codes, scale, first, list, ws + l.codes, ws + l.scale, pairs, E, l.blocks, chunk, p.tile, k, p.x_per_pair, K};
+    const int rc = mx_launch(mp_place_kernel, dim3((pairs + chunk - 1) / chunk), kMpPlaceThreads, 0, st, MpPlaceParams(pp));
     if (rc != SLICEMOE_OK) return rc;
     p.first = first;
     p.list = list;
