@@ -73,22 +73,29 @@ __host__ __device__ inline MpLayout mp_layout(int T, int k, int E, int K) {
 }
 
 // ---- pairs by expert, and their rows into tiles --------------------------------------------------------------------
-// Exclusive scan over the block of one value per thread; *total gets the sum.  s: one int per warp.
+// Exclusive scans over the block of three values per thread, side by side; total gets the sums.
 template <int THREADS>
-__device__ __forceinline__ int mp_scan(int v, int* s, int* total) {
+__device__ __forceinline__ void mp_scan3(int (&v)[3], int (*s)[3], int (&total)[3]) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int inc = v;
+  int inc[3] = {v[0], v[1], v[2]};
 #pragma unroll
   for (int off = 1; off < 32; off <<= 1) {
-    const int a = __shfl_up_sync(0xffffffffu, inc, off);
-    if (lane >= off) inc += a;
+    int a[3];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) a[i] = __shfl_up_sync(0xffffffffu, inc[i], off);
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+      if (lane >= off) inc[i] += a[i];
   }
   __syncthreads();
-  if (lane == 31) s[warp] = inc;
+  if (lane == 31) s[warp][0] = inc[0], s[warp][1] = inc[1], s[warp][2] = inc[2];
   __syncthreads();
-  const int w = lane < THREADS / 32 ? s[lane] : 0;
-  *total = __reduce_add_sync(0xffffffffu, w);
-  return __reduce_add_sync(0xffffffffu, lane < warp ? w : 0) + inc - v;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    const int w = lane < THREADS / 32 ? s[lane][i] : 0, before = lane < warp ? w : 0;
+    total[i] = __reduce_add_sync(0xffffffffu, w);
+    v[i] = __reduce_add_sync(0xffffffffu, before) + inc[i] - v[i];
+  }
 }
 
 struct MpSortParams {
@@ -135,18 +142,22 @@ struct MpPlaceParams {
   uint8_t *t_codes, *t_scale;
   int pairs, E, blocks, chunk, tile, k, x_per_pair, K;
 };
-// Each pair's row to its place in its tile; scales as those of packed weights.  A block takes `chunk` pairs of one block of ranks, a warp
-// four of them at a time: a row is read in runs of 512 bytes and written in runs of 128, which is what the swizzled operand layout
-// keeps together.  (Without the swizzle a row's pieces of 16 bytes lie apart: 9 us for 8,192 rows of 2,048 values and 28 for 49,152 of
-// 1,408, in whichever order the rows are taken.)
-constexpr int kMpPlaceRows = 4;
-__global__ void __launch_bounds__(kMpPlaceThreads) mp_place_kernel(const MpPlaceParams p) {
-  __shared__ int s_first[kMpMaxExperts], s_before[kMpMaxExperts], s_count[kMpMaxExperts], s_tile[kMpMaxExperts], s_row[kMpMaxExperts], s_sums[32];
+// Each pair's row to its place in its tile; scales as those of packed weights.  A block takes `chunk` pairs of one block of ranks: where they
+// go is worked out by a thread each, then a warp moves four rows at a time.  A row is read in runs of 512 bytes and written in runs of
+// 128, which is what the swizzled operand layout keeps together.  (Without the swizzle a row's pieces of 16 bytes lie apart: 9 us
+// for 8,192 rows of 2,048 values and 28 for 49,152 of 1,408, in whichever order the rows are taken.)
+constexpr int kMpPlaceRows = 4, kMpPlaceChunk = 128;
+struct MpPlace {
+  uint32_t x, code, scale, row;  // row of x (all ones: none); rows, and blocks of scales, before the tile; rows of the tile << 16 | row in it
+};
+__global__ void __launch_bounds__(kMpPlaceThreads, 4) mp_place_kernel(const MpPlaceParams p) {
+  __shared__ int s_first[kMpMaxExperts], s_before[kMpMaxExperts], s_count[kMpMaxExperts], s_tile[kMpMaxExperts], s_row[kMpMaxExperts], s_sums[32][3];
+  __shared__ MpPlace s_place[kMpPlaceChunk];
   mx_dep_launch();
   mx_dep_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int base = blockIdx.x * p.chunk, me = base / kMpSortPairs;
-  int rows = 0, tiles = 0, padded = 0;
+  int sum[3] = {};
   for (int e0 = 0; e0 < p.E; e0 += kMpPlaceThreads) {
     const int e = e0 + tid;
     int count = 0, before = 0;
@@ -163,79 +174,74 @@ __global__ void __launch_bounds__(kMpPlaceThreads) mp_place_kernel(const MpPlace
       }
     }
     const MpTiles t = mp_tiles(count, p.tile);
-    int total;
-    const int f = rows + mp_scan<kMpPlaceThreads>(count, s_sums, &total);
-    rows += total;
-    const int o = tiles + mp_scan<kMpPlaceThreads>(t.n, s_sums, &total);
-    tiles += total;
-    const int r = padded + mp_scan<kMpPlaceThreads>(t.n * t.each, s_sums, &total);
-    padded += total;
+    int v[3] = {count, t.n, t.n * t.each}, total[3];
+    mp_scan3<kMpPlaceThreads>(v, s_sums, total);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      v[i] += sum[i];
+      sum[i] += total[i];
+    }
     if (e < p.E) {
-      s_first[e] = f, s_before[e] = before, s_count[e] = count, s_tile[e] = o, s_row[e] = r;
-      if (blockIdx.x == 0) p.first[e] = f, p.first[p.E + 1 + e] = o, p.first[2 * (p.E + 1) + e] = r;
+      s_first[e] = v[0], s_before[e] = before, s_count[e] = count, s_tile[e] = v[1], s_row[e] = v[2];
+      if (blockIdx.x == 0) p.first[e] = v[0], p.first[p.E + 1 + e] = v[1], p.first[2 * (p.E + 1) + e] = v[2];
     }
   }
-  if (blockIdx.x == 0 && tid == 0) p.first[p.E] = rows, p.first[2 * p.E + 1] = tiles;
-  __syncthreads();
+  if (blockIdx.x == 0 && tid == 0) p.first[p.E] = sum[0], p.first[2 * p.E + 1] = sum[1];
   const int atoms = mx_atoms(p.K), pieces = 2 * mx_chunks(p.K), kbytes = p.K >> 1, halves = (p.tile + 127) >> 7, steps = mp_steps(p.K);
-  for (int i = warp * kMpPlaceRows; i < p.chunk; i += kMpPlaceThreads / 32 * kMpPlaceRows) {
-    // lane l < 4 works out where pair i + l goes
-    const int pair = base + i + lane;
-    int64_t x = -1;
-    size_t code_at = 0, scale_at = 0;
-    int each = 0, row = 0;
-    if (lane < kMpPlaceRows && pair < p.pairs) {
-      const int e = p.ids ? __ldcg(p.ids + pair) : 0;
-      if ((unsigned)e < (unsigned)p.E) {
-        const int pos = p.ids ? s_before[e] + __ldcg(p.rank + pair) : pair, count = s_count[e];
-        const MpTiles t = count <= p.tile ? MpTiles{1, (count + 15) & ~15} : mp_tiles(count, p.tile);
-        const int tile = t.n == 1 ? 0 : pos / t.each;
-        row = pos - tile * t.each;
-        each = t.each;
-        x = p.x_per_pair ? pair : pair / p.k;
-        code_at = (size_t)(s_row[e] + tile * t.each) * steps * kMpRowBytes;
-        scale_at = (size_t)(s_tile[e] + tile) * atoms * halves * kMxAtomBytes + (row >> 7) * kMxAtomBytes + (row & 31) * 16 + ((row >> 5) & 3) * 4;
-        p.list[s_first[e] + pos] = pair;
+  for (int c0 = 0; c0 < p.chunk; c0 += kMpPlaceChunk) {
+    const int here = min(kMpPlaceChunk, p.chunk - c0);
+    __syncthreads();
+    if (tid < here) {
+      const int pair = base + c0 + tid;
+      MpPlace at = {0xffffffffu, 0, 0, 0};
+      if (pair < p.pairs) {
+        const int e = p.ids ? __ldcg(p.ids + pair) : 0, rank = p.ids ? __ldcg(p.rank + pair) : pair;
+        if ((unsigned)e < (unsigned)p.E) {
+          const int pos = p.ids ? s_before[e] + rank : pair, count = s_count[e];
+          const MpTiles t = count <= p.tile ? MpTiles{1, (count + 15) & ~15} : mp_tiles(count, p.tile);
+          const int tile = t.n == 1 ? 0 : pos / t.each;
+          at.x = p.x_per_pair ? pair : pair / p.k;
+          at.code = s_row[e] + tile * t.each;
+          at.scale = s_tile[e] + tile;
+          at.row = t.each << 16 | (pos - tile * t.each);
+          p.list[s_first[e] + pos] = pair;
+        }
       }
+      s_place[tid] = at;
     }
-    int64_t xs[kMpPlaceRows];
-    size_t cs[kMpPlaceRows], ss[kMpPlaceRows];
-    int es[kMpPlaceRows], rs[kMpPlaceRows];
+    __syncthreads();
+    for (int i = warp * kMpPlaceRows; i < here; i += kMpPlaceThreads / 32 * kMpPlaceRows) {
+      // loads first, then stores: left to itself the compiler cannot know that they do not overlap, and waits for each
+      for (int q = lane; q < pieces; q += 32) {
+        uint4 v[kMpPlaceRows];
 #pragma unroll
-    for (int l = 0; l < kMpPlaceRows; ++l) {
-      xs[l] = __shfl_sync(0xffffffffu, x, l);
-      cs[l] = __shfl_sync(0xffffffffu, code_at, l);
-      ss[l] = __shfl_sync(0xffffffffu, scale_at, l);
-      es[l] = __shfl_sync(0xffffffffu, each, l);
-      rs[l] = __shfl_sync(0xffffffffu, row, l);
-    }
-    // loads first, then stores: left to itself the compiler cannot know that they do not overlap, and waits for each
-    for (int q0 = 0; q0 < pieces; q0 += 64) {
-      uint4 v[kMpPlaceRows][2];
-#pragma unroll
-      for (int l = 0; l < kMpPlaceRows; ++l)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int q = q0 + 32 * h + lane;
-          v[l][h] = xs[l] >= 0 && q * 16 < kbytes ? __ldcg(reinterpret_cast<const uint4*>(p.codes + xs[l] * kbytes) + q) : make_uint4(0, 0, 0, 0);
+        for (int l = 0; l < kMpPlaceRows; ++l) {
+          const uint32_t x = s_place[i + l].x;
+          v[l] = ~x && q * 16 < kbytes ? __ldcg(reinterpret_cast<const uint4*>(p.codes + (size_t)x * kbytes) + q) : make_uint4(0, 0, 0, 0);
         }
 #pragma unroll
-      for (int l = 0; l < kMpPlaceRows; ++l)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int q = q0 + 32 * h + lane;
-          if (xs[l] >= 0 && q < pieces) *reinterpret_cast<uint4*>(p.t_codes + cs[l] + mp_piece(es[l], rs[l], q)) = v[l][h];
+        for (int l = 0; l < kMpPlaceRows; ++l) {
+          const MpPlace at = s_place[i + l];
+          if (~at.x) *reinterpret_cast<uint4*>(p.t_codes + (size_t)at.code * steps * kMpRowBytes + mp_piece(at.row >> 16, at.row & 0xffffu, q)) = v[l];
         }
-    }
-    for (int j = lane; j < atoms; j += 32) {
-      const int left = (p.K >> 5) - 4 * j;
-      uint32_t w[kMpPlaceRows];
+      }
+      for (int j = lane; j < atoms; j += 32) {
+        const int left = (p.K >> 5) - 4 * j;
+        uint32_t w[kMpPlaceRows];
 #pragma unroll
-      for (int l = 0; l < kMpPlaceRows; ++l) w[l] = xs[l] >= 0 ? __ldcg(reinterpret_cast<const uint32_t*>(p.scale + xs[l] * (4 * atoms)) + j) : 0u;
+        for (int l = 0; l < kMpPlaceRows; ++l) {
+          const uint32_t x = s_place[i + l].x;
+          w[l] = ~x ? __ldcg(reinterpret_cast<const uint32_t*>(p.scale + (size_t)x * (4 * atoms)) + j) : 0u;
+        }
 #pragma unroll
-      for (int l = 0; l < kMpPlaceRows; ++l) {
-        if (left < 4) w[l] &= (1u << (8 * left)) - 1u;  // bytes beyond the row's end
-        if (xs[l] >= 0) *reinterpret_cast<uint32_t*>(p.t_scale + ss[l] + (size_t)j * halves * kMxAtomBytes) = w[l];
+        for (int l = 0; l < kMpPlaceRows; ++l) {
+          const MpPlace at = s_place[i + l];
+          const uint32_t r = at.row & 0xffffu;
+          if (left < 4) w[l] &= (1u << (8 * left)) - 1u;  // bytes beyond the row's end
+          if (~at.x)
+            *reinterpret_cast<uint32_t*>(p.t_scale + (((size_t)at.scale * atoms + j) * halves + (r >> 7)) * kMxAtomBytes + (r & 31) * 16 +
+                                         ((r >> 5) & 3) * 4) = w[l];
+        }
       }
     }
   }
@@ -876,7 +882,7 @@ extern "C" int slicemoe_mx4_product(const slicemoe_mx4_mat* mats, int n_experts,
       if (rc != SLICEMOE_OK) return rc;
     }
     int chunk = kMpPlaceThreads / 32 * kMpPlaceRows;  // pairs of a block: more where there are blocks enough to fill the device
-    while (chunk < kMpSortPairs && pairs / chunk > 148 * 4) chunk *= 2;
+    while (chunk < kMpSortPairs && pairs / chunk > 148 * 6) chunk *= 2;
     const MpPlaceParams pp = {ids, rank, hist, codes, scale, first, list, ws + l.codes, ws + l.scale, pairs, E, l.blocks, chunk, p.tile, k, p.x_per_pair, K};
     const int rc = mx_launch(mp_place_kernel, dim3((pairs + chunk - 1) / chunk), kMpPlaceThreads, 0, st, MpPlaceParams(pp));
     if (rc != SLICEMOE_OK) return rc;
