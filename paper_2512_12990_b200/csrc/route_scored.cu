@@ -1,22 +1,27 @@
 // slicemoe_route_scored: softmax or sigmoid scores, a bias for balance, groups of experts, top-k.  One warp per token.
 //
-// Lane l holds experts l, l + 32, ...  Without a bias experts are ordered by their logits, which is exact.  With one the key is
-// score + bias, first in fp32: every key is within kNear / 2 of its value (below), so two keys further apart than kNear are in
-// their true order.  Where a choice hangs on two that are nearer - about one token in a thousand for keys spread like those of 256
-// experts - the warp works out the token's keys again in fp64 and chooses by those.  The same for groups' values, sums of keys.
+// Lane l holds the VPT consecutive experts from l VPT on.  Without a bias experts are ordered by their logits, which is exact.  With
+// one the key is score + bias, first in fp32: keys further apart than kNear are in their true order.  Where a choice hangs on two
+// that are nearer - about one token in a thousand for keys spread like those of 256 experts - the warp works out the token's keys again
+// in fp64 and chooses by those.  The same for groups' values, sums of keys.
+//
+// What counts is the number of instructions (8,192 tokens of 256 experts are 8 MB, 1.3 us of reading).  A lane sorts its keys once; a round
+// of the selection is then a warp maximum of the lanes' first keys, a ballot for the lowest lane that has it, and a shift in that
+// lane.  Which expert a selected key belongs to is looked up at the end, for all selections side by side.  A group that is made of
+// whole lanes has its two largest keys from the sorted ones by exchanges, and is kept or dropped by lanes.  (Rounds that look through
+// all of a lane's keys, and groups scanned in shared memory, took 1,930 instructions a token and 30 us.)
 #include "mx4.cuh"
 #include "route.cuh"
 
 namespace slicemoe {
 
-// Error of an fp32 key.  expf is off by 2 ulp, 2^-22 relative.  Sigmoid s = 1 / (1 + t): ds = s (1 - s) dt / t <= 2^-24, the
-// sum and the quotient round by 2^-24 each, s <= 1: below 2^-22.4.  Softmax p = e^-d / sum: d rounds by 2^-24 d and
-// d e^-d < 0.37; expf's 2^-22 and the sum's (16 terms in a row, then 5 exchanges; at most 21 roundings of 2^-24, and expf's), the
-// reciprocal and the product 2^-24 each: below (2^-22 + 2^-22 + 24 x 2^-24) p + 0.37 x 2^-24 < 2^-18.9 p.  Adding the bias rounds by
-// 2^-24 |key|.  Two keys' errors, with room: 2^-20.5 for sigmoids, 2^-17.8 max p for softmax; both by kNear = 2^-20 and 2^-17,
-// times max(1, |key|).  A group's value of two keys: twice that.
-constexpr float kNearSigmoid = 9.5367431640625e-7f, kNearSoftmax = 7.62939453125e-6f;
-constexpr int kRsWarps = 4;       // tokens of a block
+// Error of an fp32 key.  Sigmoid s = 1 / (1 + t), t = __expf(-l), off by (2 + 1.2 |l|) 2^-23 relative, which enters s with s (1 - s):
+// below 0.6 x 2^-23 for every l; 1 + t rounds by 2^-24 s, __fdividef by 2 ulp, 2^-22 s; adding the bias by 2^-24 |key|: below
+// 2^-21.1 max(1, |key|), two keys 2^-20.1.  Softmax p = e^-d / sum: d rounds by 2^-24 d and d e^-d < 0.37; expf's 2 ulp and the sum's (16 terms
+// in a row, then 5 exchanges: at most 21 roundings of 2^-24, and expf's), the reciprocal and the product 2^-24 each: below 2^-18.9 p +
+// 0.37 x 2^-24, two keys 2^-17.8.  A group's value of two keys: twice that.
+constexpr float kNearSigmoid = 9.5367431640625e-7f, kNearSoftmax = 7.62939453125e-6f;  // 2^-20, 2^-17; times max(1, |key|)
+constexpr int kRsWarps = 4;
 constexpr int kRsMaxGroups = 32;
 
 struct RsParams {
@@ -26,7 +31,9 @@ struct RsParams {
   int32_t* ids;
   float* weights;
   uint8_t* prec_req;
-  int T, E, k, dtype, n_group, topk_group, group_best, lanes;  // lanes: that share a group, a power of two
+  int T, E, k, dtype, n_group, topk_group, group_best;
+  int lanes;    // that share a group: of whole lanes, a power of two; 0: groups are scanned in shared memory
+  int wide;     // a lane's logits are loaded 16 bytes at a time
   int renorm, rank_high;
   float scale, tau, inv_size;
 };
@@ -39,12 +46,38 @@ __device__ __forceinline__ float rs_logit(const RsParams& p, int64_t at) {
     v = mx_load(static_cast<const __nv_bfloat16*>(p.logits) + at);
   else
     v = mx_load(static_cast<const __half*>(p.logits) + at);
-  return isnan(v) ? -CUDART_INF_F : v;
+  return v;
+}
+// A lane's logits as they are in memory; those of experts that do not exist are -inf.
+template <int VPT>
+__device__ __forceinline__ void rs_load(const RsParams& p, int t, int lane, float (&val)[VPT]) {
+  const int64_t at = t * p.ld + lane * VPT;
+  if (VPT >= 8 && p.wide) {
+#pragma unroll
+    for (int v = 0; v < VPT; v += 8) {
+      float f[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] = -CUDART_INF_F;
+      if (lane * VPT + v < p.E) {
+        if (p.dtype == SLICEMOE_F32)
+          mx_load8<float, true>(static_cast<const float*>(p.logits) + at + v, f);
+        else if (p.dtype == SLICEMOE_BF16)
+          mx_load8<__nv_bfloat16, true>(static_cast<const __nv_bfloat16*>(p.logits) + at + v, f);
+        else
+          mx_load8<__half, true>(static_cast<const __half*>(p.logits) + at + v, f);
+      }
+#pragma unroll
+      for (int i = 0; i < 8 && v + i < VPT; ++i) val[v + i] = f[i];
+    }
+  } else {
+#pragma unroll
+    for (int v = 0; v < VPT; ++v) val[v] = lane * VPT + v < p.E ? rs_logit(p, at + v) : -CUDART_INF_F;
+  }
 }
 
 // Keys as unsigned integers of the same order; 0 stands for no key (below that of -inf).
 __device__ __forceinline__ uint32_t rs_ordered(float k) {
-  const uint32_t b = __float_as_uint(isnan(k) ? -CUDART_INF_F : k + 0.0f);
+  const uint32_t b = __float_as_uint(k + 0.0f);
   return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float rs_value(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o); }
@@ -55,7 +88,6 @@ __device__ __forceinline__ uint64_t rs_ordered(double k) {
 __device__ __forceinline__ double rs_value(uint64_t o) {
   return __longlong_as_double((long long)(o & 0x8000000000000000ull ? o ^ 0x8000000000000000ull : ~o));
 }
-__device__ __forceinline__ uint32_t rs_warp_max(uint32_t v) { return __reduce_max_sync(0xffffffffu, v); }
 __device__ __forceinline__ uint64_t rs_warp_max(uint64_t v) {
   const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(v >> 32));
   const uint32_t lo = __reduce_max_sync(0xffffffffu, (uint32_t)(v >> 32) == hi ? (uint32_t)v : 0u);
@@ -66,14 +98,15 @@ __device__ __forceinline__ bool rs_near(float a, float b, float near) {
   return !(a - b > near * fmaxf(1.0f, fmaxf(fabsf(a), fabsf(b)))) && !(isinf(a) && isinf(b));
 }
 
-// Which groups are kept, as a bit mask.  keys: the token's, in shared memory; F: their type.  `lanes` lanes scan a group each; a
-// group's value is then in the first of them.
+// Which groups are kept, as a bit mask, from the token's keys (of type F) in shared memory: `share` lanes scan a group each.
 template <class F>
 __device__ __forceinline__ uint32_t rs_groups(const RsParams& p, const F* keys, int lane, float near, bool* unsure) {
-  const int size = p.E / p.n_group, g = lane / p.lanes;
+  int share = 1;
+  while (share * 2 * p.n_group <= 32) share *= 2;
+  const int size = p.E / p.n_group, g = lane / share;
   F b0 = (F)-CUDART_INF_F, b1 = (F)-CUDART_INF_F;
   if (g < p.n_group)
-    for (int i = lane % p.lanes; i < size; i += p.lanes) {
+    for (int i = lane % share; i < size; i += share) {
       const F v = keys[g * size + i];
       if (v > b0) {
         b1 = b0;
@@ -82,7 +115,7 @@ __device__ __forceinline__ uint32_t rs_groups(const RsParams& p, const F* keys, 
         b1 = v;
       }
     }
-  for (int off = 1; off < p.lanes; off <<= 1) {
+  for (int off = 1; off < share; off <<= 1) {
     const F o0 = __shfl_xor_sync(0xffffffffu, b0, off), o1 = __shfl_xor_sync(0xffffffffu, b1, off);
     b1 = fmax(fmin(b0, o0), b0 >= o0 ? b1 : o1);
     b0 = fmax(b0, o0);
@@ -91,202 +124,343 @@ __device__ __forceinline__ uint32_t rs_groups(const RsParams& p, const F* keys, 
   if (isnan(mine)) mine = (F)-CUDART_INF_F;
   int rank = 0;
   for (int o = 0; o < p.n_group; ++o) {
-    const F v = __shfl_sync(0xffffffffu, mine, o * p.lanes);
+    const F v = __shfl_sync(0xffffffffu, mine, o * share);
     rank += v > mine || (v == mine && o < g);
   }
-  const bool mine_counts = g < p.n_group && lane % p.lanes == 0;
-  const bool kept = mine_counts && rank < p.topk_group;
+  const bool counts = g < p.n_group && lane % share == 0, kept = counts && rank < p.topk_group;
   if (unsure) {
-    F low = kept ? mine : (F)CUDART_INF_F, high = mine_counts && !kept ? mine : (F)-CUDART_INF_F;
+    F low = kept ? mine : (F)CUDART_INF_F, high = counts && !kept ? mine : (F)-CUDART_INF_F;
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) {
-      low = fmin(low, __shfl_xor_sync(0xffffffffu, low, off));
-      high = fmax(high, __shfl_xor_sync(0xffffffffu, high, off));
+      const F l = __shfl_xor_sync(0xffffffffu, low, off), h = __shfl_xor_sync(0xffffffffu, high, off);
+      low = fmin(low, l);
+      high = fmax(high, h);
     }
     *unsure = p.topk_group < p.n_group && rs_near((float)low, (float)high, 2.0f * near);
   }
-  uint32_t mask = __ballot_sync(0xffffffffu, kept);
-  if (p.lanes > 1) {  // bit of group g from lane g * lanes
-    uint32_t m = 0;
-    for (int o = 0; o < p.n_group; ++o) m |= ((mask >> (o * p.lanes)) & 1u) << o;
-    mask = m;
-  }
+  const uint32_t lanes = __ballot_sync(0xffffffffu, kept);  // bit of group g from lane g * share
+  uint32_t mask = 0;
+  for (int o = 0; o < p.n_group; ++o) mask |= ((lanes >> (o * share)) & 1u) << o;
   return mask;
 }
-
-// k rounds of the largest key, the lowest index that has it.  Lane j < k gets selection j.  `near` >= 0: *unsure is set where two
-// selections in a row, or the last and the best that is left, are too near.
-template <class U, int VPT>
-__device__ __forceinline__ int rs_select(U (&key)[VPT], int k, int left, int lane, float near, bool* unsure) {
-  int idsel = 0;
-  float last = 0.0f;
-  const int rounds = unsure && k < left ? k + 1 : k;
-  for (int j = 0; j < rounds; ++j) {
-    U best = key[0];
-    int bv = 0;
-#pragma unroll
-    for (int v = 1; v < VPT; ++v)
-      if (key[v] > best) {
-        best = key[v];
-        bv = v;
-      }
-    const U top = rs_warp_max(best);
-    if (unsure) {
-      const float t = (float)rs_value(top);
-      if (j > 0 && rs_near(last, t, near)) *unsure = true;
-      last = t;
-    }
-    if (j == k) break;
-    const int e = (int)__reduce_min_sync(0xffffffffu, best == top ? (uint32_t)(bv * 32 + lane) : 0xffffffffu);
-#pragma unroll
-    for (int v = 0; v < VPT; ++v)
-      if (e == v * 32 + lane) key[v] = 0;
-    if (lane == j) idsel = e;
-  }
-  return idsel;
+__device__ __forceinline__ bool rs_kept(const RsParams& p, uint32_t kept, int e) {
+  return (kept >> (int)(((float)e + 0.5f) * p.inv_size)) & 1u;
 }
 
-// The same choice with keys in 64 bits.
-template <int VPT, bool SIGMOID>
-__device__ __noinline__ int rs_exact(const RsParams& p, const float (&val)[VPT], float vmax, double* keys, int lane) {
-  double s[VPT], sum = 0.0;
-#pragma unroll
-  for (int v = 0; v < VPT; ++v) {
-    const int e = v * 32 + lane;
-    if constexpr (SIGMOID) {
-      s[v] = 1.0 / (1.0 + exp(-(double)val[v]));
-    } else {
-      s[v] = val[v] == vmax ? 1.0 : exp((double)val[v] - (double)vmax);
-      if (vmax == -CUDART_INF_F || e >= p.E) s[v] = 0.0;
-      sum += s[v];
-    }
-  }
+// A score in 64 bits; total: the sum that a softmax divides by.
+template <bool SIGMOID>
+__device__ __forceinline__ double rs_score(float l, float vmax, double total) {
+  if constexpr (SIGMOID) return 1.0 / (1.0 + exp(-(double)l));
+  return total > 0.0 ? (l == vmax ? 1.0 : exp((double)l - (double)vmax)) / total : 0.0;
+}
+template <bool SIGMOID>
+__device__ __forceinline__ double rs_total(const RsParams& p, const float* logits, float vmax, int lane) {
+  double total = 0.0;
   if constexpr (!SIGMOID) {
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-  }
-  uint64_t key[VPT];
-#pragma unroll
-  for (int v = 0; v < VPT; ++v) {
-    const int e = v * 32 + lane;
-    key[v] = 0;
-    if (e >= p.E) continue;
-    const double score = SIGMOID ? s[v] : (sum > 0.0 ? s[v] / sum : 0.0);
-    const double kk = p.bias ? score + (double)__ldcg(p.bias + e) : score;
-    key[v] = rs_ordered(kk);
-    keys[e] = rs_value(key[v]);
-  }
-  if (p.n_group > 1) {
-    __syncwarp();
-    const uint32_t kept = rs_groups(p, (const double*)keys, lane, 0.0f, nullptr);
-#pragma unroll
-    for (int v = 0; v < VPT; ++v) {
-      const int e = v * 32 + lane;
-      if (e < p.E && !((kept >> (int)(((float)e + 0.5f) * p.inv_size)) & 1u)) key[v] = 0;
+    if (vmax > -CUDART_INF_F) {
+#pragma unroll 1
+      for (int e = lane; e < p.E; e += 32) total += logits[e] == vmax ? 1.0 : exp((double)logits[e] - (double)vmax);
     }
-  }
-  if (!p.bias) {  // within the groups the logits' order is exact, and finer than that of their scores
 #pragma unroll
-    for (int v = 0; v < VPT; ++v)
-      if (key[v]) key[v] = rs_ordered((double)val[v]);
+    for (int off = 16; off > 0; off >>= 1) total += __shfl_xor_sync(0xffffffffu, total, off);
   }
-  return rs_select<uint64_t, VPT>(key, p.k, 0, lane, 0.0f, nullptr);
+  return total;
+}
+
+// Both of the following are made of small loops: they run for few tokens, and instructions that have to be fetched first are what they
+// would otherwise wait for (with everything unrolled one such token took 10 us).
+
+// The order of the first `n` candidates (lane j holds one, id) by their keys in 64 bits; lane j gets the j-th of them.
+template <bool SIGMOID>
+__device__ __noinline__ int rs_reorder(const RsParams& p, const float* logits, float vmax, int id, int n, int lane) {
+  const double total = rs_total<SIGMOID>(p, logits, vmax, lane);
+  double key = -CUDART_INF;
+  if (lane < n) key = rs_score<SIGMOID>(logits[id], vmax, total) + (double)__ldcg(p.bias + id);
+  if (isnan(key)) key = -CUDART_INF;
+  int rank = 0;
+#pragma unroll 1
+  for (int j = 0; j < n; ++j) {
+    const double k = __shfl_sync(0xffffffffu, key, j);
+    const int i = __shfl_sync(0xffffffffu, id, j);
+    rank += k > key || (k == key && i < id);
+  }
+  int mine = 0;
+#pragma unroll 1
+  for (int j = 0; j < n; ++j) {  // the candidate of rank `lane`
+    const int r = __shfl_sync(0xffffffffu, rank, j), i = __shfl_sync(0xffffffffu, id, j);
+    if (r == lane) mine = i;
+  }
+  return mine;
+}
+
+// The whole choice with keys in 64 bits: k rounds of the largest key, the lowest index that has it.  Lane j < k gets selection j.
+template <bool SIGMOID>
+__device__ __noinline__ int rs_exact(const RsParams& p, const float* logits, double* keys, float vmax, int lane) {
+  const double total = rs_total<SIGMOID>(p, logits, vmax, lane);
+#pragma unroll 1
+  for (int e = lane; e < p.E; e += 32) {
+    double key = rs_score<SIGMOID>(logits[e], vmax, total);
+    if (p.bias) key += (double)__ldcg(p.bias + e);
+    keys[e] = isnan(key) ? -CUDART_INF : key;
+  }
+  __syncwarp();
+  uint32_t kept = 0xffffffffu;
+  if (p.n_group > 1) kept = rs_groups(p, (const double*)keys, lane, 0.0f, nullptr);
+  __syncwarp();
+#pragma unroll 1
+  for (int e = lane; e < p.E; e += 32) {
+    if (!p.bias) keys[e] = (double)logits[e];  // within the groups the logits' order is exact, and finer than that of their scores
+    if (p.n_group > 1 && !rs_kept(p, kept, e)) keys[e] = CUDART_NAN;  // out of the choice
+  }
+  int id = 0;
+#pragma unroll 1
+  for (int j = 0; j < p.k; ++j) {
+    uint64_t best = 0;
+    int at = 0;
+#pragma unroll 1
+    for (int e = lane; e < p.E; e += 32) {
+      const double v = keys[e];
+      const uint64_t o = isnan(v) ? 0ull : rs_ordered(v);
+      if (o > best) best = o, at = e;
+    }
+    const uint64_t top = rs_warp_max(best);
+    const int e = (int)__reduce_min_sync(0xffffffffu, best == top ? (uint32_t)at : 0xffffffffu);
+    if ((e & 31) == lane) keys[e] = CUDART_NAN;
+    if (lane == j) id = e;
+  }
+  return id;
+}
+
+// Descending, by an odd-even merge network.
+template <int N>
+__device__ __forceinline__ void rs_sort(uint32_t (&a)[N]) {
+#pragma unroll
+  for (int p = 1; p < N; p <<= 1)
+#pragma unroll
+    for (int k = p; k >= 1; k >>= 1)
+#pragma unroll
+      for (int j = k % p; j + k < N; j += 2 * k)
+#pragma unroll
+        for (int i = 0; i < k; ++i)
+          if (i + j + k < N && (i + j) / (2 * p) == (i + j + k) / (2 * p)) {
+            const uint32_t x = a[i + j], y = a[i + j + k];
+            a[i + j] = max(x, y);
+            a[i + j + k] = min(x, y);
+          }
 }
 
 template <int VPT, bool SIGMOID>
-__global__ void __launch_bounds__(32 * kRsWarps) route_scored_kernel(const RsParams p) {
-  __shared__ double s_keys[kRsWarps][32 * VPT];
+__global__ void __launch_bounds__(32 * kRsWarps, VPT <= 8 ? 8 : 4) route_scored_kernel(const RsParams p) {
+  __shared__ __align__(16) double s_keys[kRsWarps][32 * VPT];  // a token's keys in 32 bits, or in 64
+  __shared__ __align__(16) float s_logits[kRsWarps][32 * VPT];
   mx_dep_launch();
   mx_dep_wait();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t = blockIdx.x * kRsWarps + warp;
-  if (t >= p.T) return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   constexpr float near = SIGMOID ? kNearSigmoid : kNearSoftmax;
-  float val[VPT], vmax = -CUDART_INF_F;
+  uint32_t* keys = reinterpret_cast<uint32_t*>(s_keys[warp]);
+  float* logits = s_logits[warp];
+  const int stride = gridDim.x * kRsWarps;
+  int t = blockIdx.x * kRsWarps + warp;
+  float bias[VPT], ahead[VPT];
+  if (t < p.T) rs_load<VPT>(p, t, lane, ahead);
+  if (p.bias) {
+    // read once a block, in whole lines: the same kilobyte read by every warp for itself, eight values apart, kept a few L2 slices busy
+    // for 19 of 28 us (8,192 tokens of 256 experts)
+    float* all = s_logits[0];
+    for (int e = threadIdx.x; e < 32 * VPT; e += 32 * kRsWarps) all[e] = e < p.E ? __ldcg(p.bias + e) : 0.0f;
+    __syncthreads();
 #pragma unroll
-  for (int v = 0; v < VPT; ++v) {
-    const int e = v * 32 + lane;
-    val[v] = e < p.E ? rs_logit(p, t * p.ld + e) : -CUDART_INF_F;
-    vmax = fmaxf(vmax, val[v]);
+    for (int v = 0; v < VPT; ++v) bias[v] = all[lane * VPT + v];
+    __syncthreads();
   }
-  float inv_sum = 0.0f;
-  if constexpr (!SIGMOID) {
-    asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(vmax) : "f"(vmax));
-    float sum = 0.0f;
-    if (vmax > -CUDART_INF_F) {
+  if (t >= p.T) return;
+  for (; t < p.T; t += stride) {
+    float val[VPT], vmax = -CUDART_INF_F;
 #pragma unroll
-      for (int v = 0; v < VPT; ++v)
-        if (v * 32 + lane < p.E) sum += val[v] == vmax ? 1.0f : expf(val[v] - vmax);
+    for (int v = 0; v < VPT; ++v) val[v] = isnan(ahead[v]) ? -CUDART_INF_F : ahead[v];
+    if (t + stride < p.T) rs_load<VPT>(p, t + stride, lane, ahead);  // the next token's are on their way meanwhile
+    float inv_sum = 0.0f;
+    if constexpr (!SIGMOID) {
+#pragma unroll
+      for (int v = 0; v < VPT; ++v) vmax = fmaxf(vmax, val[v]);
+      asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(vmax) : "f"(vmax));
+      float sum = 0.0f;
+      if (vmax > -CUDART_INF_F) {
+#pragma unroll
+        for (int v = 0; v < VPT; ++v) sum += val[v] == vmax ? 1.0f : expf(val[v] - vmax);  // 0 for an expert that does not exist
+      }
+#pragma unroll
+      for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+      inv_sum = sum > 0.0f ? 1.0f / sum : 0.0f;
     }
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-    inv_sum = sum > 0.0f ? 1.0f / sum : 0.0f;
-  }
-  auto score = [&](float l) -> float {
-    if constexpr (SIGMOID) return 1.0f / (1.0f + expf(-l));
-    return (l == vmax ? 1.0f : expf(l - vmax)) * inv_sum;
-  };
-  uint32_t key[VPT];
-  float* keys = reinterpret_cast<float*>(s_keys[warp]);
-  const bool sums = p.n_group > 1 && (p.bias || p.group_best > 1);  // groups' values are of scores, not of logits
-#pragma unroll
-  for (int v = 0; v < VPT; ++v) {
-    const int e = v * 32 + lane;
-    key[v] = 0;
-    if (e >= p.E) continue;
-    float kk = val[v];
-    if (p.bias || sums) {
-      const float s = score(val[v]);
-      const float b = p.bias ? __fadd_rn(s, __ldcg(p.bias + e)) : s;
-      if (p.bias) kk = b;
-      if (p.n_group > 1) keys[e] = isnan(b) ? -CUDART_INF_F : b;
-    } else if (p.n_group > 1) {
-      keys[e] = kk;
-    }
-    key[v] = rs_ordered(kk);
-  }
-  bool unsure = false;
-  if (p.n_group > 1) {
-    __syncwarp();
-    const uint32_t kept = rs_groups(p, (const float*)keys, lane, near, sums ? &unsure : nullptr);
+    auto score = [&](float l) -> float {
+      if constexpr (SIGMOID) return __fdividef(1.0f, 1.0f + __expf(-l));
+      return (l == vmax ? 1.0f : expf(l - vmax)) * inv_sum;
+    };
+    uint32_t key[VPT];
 #pragma unroll
     for (int v = 0; v < VPT; ++v) {
-      const int e = v * 32 + lane;
-      if (e < p.E && !((kept >> (int)(((float)e + 0.5f) * p.inv_size)) & 1u)) key[v] = 0;
+      float kk = val[v];
+      if (p.bias) {
+        kk = __fadd_rn(score(val[v]), bias[v]);
+        if (isnan(kk)) kk = -CUDART_INF_F;
+      }
+      key[v] = lane * VPT + v < p.E ? rs_ordered(kk) : 0u;
     }
-  }
-  int id = rs_select<uint32_t, VPT>(key, p.k, p.topk_group * (p.E / p.n_group), lane, near, p.bias ? &unsure : nullptr);
-  if (unsure) {  // the same in all lanes
-    __syncwarp();
-    id = rs_exact<VPT, SIGMOID>(p, val, vmax, s_keys[warp], lane);
-  }
-  float l = 0.0f;  // the selection's logit, from the lane that holds it
+    __syncwarp();  // the token before is done with the arrays
 #pragma unroll
-  for (int v = 0; v < VPT; ++v) {
-    const float got = __shfl_sync(0xffffffffu, val[v], id & 31);
-    if ((id >> 5) == v) l = got;
-  }
-  const float s = lane < p.k ? score(l) : 0.0f;
-  float w = s;
-  if (p.renorm) {
-    float total = 0.0f;
-    for (int j = 0; j < p.k; ++j) total += __shfl_sync(0xffffffffu, s, j);
-    w = total > 0.0f ? s / total : 0.0f;
-  }
-  if (lane < p.k) {
-    const int64_t o = (int64_t)t * p.k + lane;
-    p.ids[o] = id;
-    p.weights[o] = w * p.scale;
-    if (p.prec_req) p.prec_req[o] = (uint8_t)(s >= p.tau || lane < p.rank_high);
+    for (int v = 0; v < VPT; v += 2) {
+      *reinterpret_cast<uint2*>(keys + lane * VPT + v) = make_uint2(key[v], key[v + 1]);
+      *reinterpret_cast<float2*>(logits + lane * VPT + v) = make_float2(val[v], val[v + 1]);
+    }
+    uint32_t (&a)[VPT] = key;
+    bool unsure = false;
+    if (p.n_group > 1 && p.lanes == 0) {
+      __syncwarp();
+      // values of groups as floats, in the logits' place
+      const bool sums = p.bias || p.group_best > 1;  // of scores, not of logits
+#pragma unroll
+      for (int v = 0; v < VPT; ++v)
+        logits[lane * VPT + v] = p.bias ? rs_value(key[v]) : (sums ? score(val[v]) : val[v]);
+      __syncwarp();
+      const uint32_t kept = rs_groups(p, (const float*)logits, lane, near, sums ? &unsure : nullptr);
+      __syncwarp();
+#pragma unroll
+      for (int v = 0; v < VPT; ++v) {
+        logits[lane * VPT + v] = val[v];
+        if (lane * VPT + v < p.E && !rs_kept(p, kept, lane * VPT + v)) a[v] = keys[lane * VPT + v] = 0u;
+      }
+    }
+    rs_sort<VPT>(a);
+    if (p.n_group > 1 && p.lanes > 0) {
+      // a group's two largest keys, in all of its lanes
+      uint32_t b0 = a[0], b1 = VPT > 1 ? a[VPT > 1 ? 1 : 0] : 0u;
+      for (int off = 1; off < p.lanes; off <<= 1) {
+        const uint32_t o0 = __shfl_xor_sync(0xffffffffu, b0, off), o1 = __shfl_xor_sync(0xffffffffu, b1, off);
+        b1 = max(min(b0, o0), max(b1, o1));
+        b0 = max(b0, o0);
+      }
+      float mine = rs_value(b0);
+      const bool sums = p.bias || p.group_best > 1;
+      if (p.group_best > 1) {
+        const float second = rs_value(b1);
+        mine = p.bias ? mine + second : score(mine) + score(second);
+      }
+      const int size = p.lanes, groups = p.n_group;
+      const bool real = lane < groups * size;
+      const uint32_t order = real ? rs_ordered(isnan(mine) ? -CUDART_INF_F : mine) : 0u;
+      int rank = 0;
+      const int me = lane / size;
+      for (int o = 0; o < groups; ++o) {
+        const uint32_t v = __shfl_sync(0xffffffffu, order, o * size);
+        rank += v > order || (v == order && o < me);
+      }
+      const bool kept = real && rank < p.topk_group;
+      if (sums && p.topk_group < groups) {
+        const uint32_t low = __reduce_min_sync(0xffffffffu, kept ? order : 0xffffffffu), high = __reduce_max_sync(0xffffffffu, kept ? 0u : order);
+        unsure = rs_near(rs_value(low), rs_value(high), 2.0f * near);
+      }
+      if (!kept) {
+#pragma unroll
+        for (int v = 0; v < VPT; ++v) a[v] = 0u;
+      }
+    }
+    // k rounds, and with a bias one more, to see how near the best that is left is
+    uint32_t my_top = 0u;
+    int my_owner = 0;
+    auto choose = [&](int j) {
+      const uint32_t top = __reduce_max_sync(0xffffffffu, a[0]);
+      const int owner = __ffs(__ballot_sync(0xffffffffu, a[0] == top)) - 1;
+      if (lane == j) my_top = top, my_owner = owner;
+      if (lane == owner) {
+#pragma unroll
+        for (int v = 0; v + 1 < VPT; ++v) a[v] = a[v + 1];
+        a[VPT - 1] = 0u;
+      }
+    };
+    int chosen = p.k + (p.bias != nullptr);
+    for (int j = 0; j < chosen; ++j) choose(j);
+    uint32_t next = __shfl_down_sync(0xffffffffu, my_top, 1);
+    bool close = false, all = unsure;  // whether selections have to be put in order, or the whole choice made again, in 64 bits
+    if (p.bias && !all) {
+      close = __any_sync(0xffffffffu, lane < p.k && next != 0u && rs_near(rs_value(my_top), rs_value(next), near));
+      if (close) {  // more candidates, until the last is clearly behind the k-th
+        const float kth = rs_value(__shfl_sync(0xffffffffu, my_top, p.k - 1));
+        for (;;) {
+          const uint32_t last = __shfl_sync(0xffffffffu, my_top, chosen - 1);
+          if (last == 0u || !rs_near(kth, rs_value(last), near)) break;
+          if (chosen == 32) {
+            all = true;
+            break;
+          }
+          choose(chosen++);
+        }
+        next = __shfl_down_sync(0xffffffffu, my_top, 1);
+      }
+    }
+    int id;
+    if (all) {  // the same in all lanes
+      __syncwarp();
+      id = rs_exact<SIGMOID>(p, logits, s_keys[warp], vmax, lane);
+    } else {
+      const bool tied = __any_sync(0xffffffffu, lane + 1 < chosen && next == my_top);
+      int skip = 0;  // of equal keys in one lane, which one
+      if (tied) {
+        const unsigned same = __match_any_sync(0xffffffffu, my_top), lanes = __match_any_sync(0xffffffffu, my_owner);
+        skip = __popc(same & lanes & ((1u << lane) - 1u));
+      }
+      __syncwarp();
+      id = my_owner * VPT;
+#pragma unroll
+      for (int v = VPT - 1; v >= 0; --v)
+        if (keys[my_owner * VPT + v] == my_top) id = my_owner * VPT + v;
+      if (tied) {
+        for (int v = 0; v < VPT; ++v)
+          if (keys[my_owner * VPT + v] == my_top && skip-- == 0) id = my_owner * VPT + v;
+      }
+      if (close) {
+        const int n = __popc(__ballot_sync(0xffffffffu, lane < chosen && my_top != 0u));
+        id = rs_reorder<SIGMOID>(p, logits, vmax, id, n, lane);
+      }
+    }
+    __syncwarp();
+    const float l = logits[min(id, p.E - 1)];
+    float s = 0.0f;
+    if (lane < p.k) {
+      if constexpr (SIGMOID)
+        s = 1.0f / (1.0f + expf(-l));
+      else
+        s = score(l);
+    }
+    float w = s;
+    if (p.renorm) {
+      float total = s;
+#pragma unroll
+      for (int off = 8; off > 0; off >>= 1) total += __shfl_xor_sync(0xffffffffu, total, off);
+      w = total > 0.0f ? s / total : 0.0f;
+    }
+    if (lane < p.k) {
+      const int64_t o = (int64_t)t * p.k + lane;
+      p.ids[o] = id;
+      p.weights[o] = w * p.scale;
+      if (p.prec_req) p.prec_req[o] = (uint8_t)(s >= p.tau || lane < p.rank_high);
+    }
   }
 }
 
 template <bool SIGMOID>
-static int rs_launch(const RsParams& p, cudaStream_t st) {
+static int rs_launch(RsParams p, cudaStream_t st) {
   void (*kernel)(RsParams) = p.E <= 64    ? route_scored_kernel<2, SIGMOID>
                              : p.E <= 128 ? route_scored_kernel<4, SIGMOID>
                              : p.E <= 256 ? route_scored_kernel<8, SIGMOID>
                                           : route_scored_kernel<16, SIGMOID>;
-  return mx_launch(kernel, dim3((p.T + kRsWarps - 1) / kRsWarps), 32 * kRsWarps, 0, st, RsParams(p));
+  const int vpt = p.E <= 64 ? 2 : p.E <= 128 ? 4 : p.E <= 256 ? 8 : 16, size = p.E / p.n_group;
+  const size_t elem = mx_elem(p.dtype);
+  p.wide = vpt >= 8 && p.E % 8 == 0 && mx_aligned(p.logits, 16) && p.ld * elem % 16 == 0;
+  p.lanes = 0;
+  if (size % vpt == 0 && ((size / vpt) & (size / vpt - 1)) == 0) p.lanes = size / vpt;
+  const int blocks = (p.T + kRsWarps - 1) / kRsWarps, most = 148 * (vpt <= 8 ? 8 : 4);  // as many as are resident together
+  return mx_launch(kernel, dim3(blocks < most ? blocks : most), 32 * kRsWarps, 0, st, RsParams(p));
 }
 
 }  // namespace slicemoe
@@ -316,8 +490,6 @@ extern "C" int slicemoe_route_scored(const void* logits, int dtype, int T, int E
   p.n_group = n_group;
   p.topk_group = topk_group;
   p.group_best = group_best;
-  p.lanes = 1;
-  while (p.lanes * 2 * n_group <= 32) p.lanes *= 2;
   p.renorm = renorm;
   p.rank_high = rank_high;
   p.scale = scale;
