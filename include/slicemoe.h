@@ -435,7 +435,7 @@ int slicemoe_route_scored(const void *logits, int dtype, int T, int E, int64_t l
  * slicemoe_mx4_dequantize - the values again, into out [rows, K] of `dtype`, rows ld elements apart (bf16 and fp32 hold every value
  * exactly; fp16 rounds, and overflows beyond 65504).
  *   K % 32 == 0; codes 16-byte, scale 4-byte aligned; x and out aligned to their element type.
- * Errors: INVALID_ARG (null, rows <= 0, K <= 0, K % 32, ld < K, alignment), UNSUPPORTED (dtype), CUDA.
+ * Errors: INVALID_ARG (null, rows <= 0, K <= 0, K % 32, ld < K, alignment), UNSUPPORTED (dtype; rows * ceil(K / 256) of 2^36 and more), CUDA.
  */
 size_t slicemoe_mx4_scale_pitch(int K);
 int slicemoe_mx4_quantize(const void *x, int dtype, int rows, int K, int64_t ld, uint8_t *codes, uint8_t *scale, void *stream);

@@ -1,4 +1,6 @@
 // slicemoe_combine: out[t] = base[t] + sum_j weights[t, j] rows[t, j].
+#include <type_traits>
+
 #include "mx4.cuh"
 
 namespace slicemoe {
@@ -13,58 +15,82 @@ struct CbParams {
 };
 constexpr int kCbThreads = 256;
 
-// A thread per eight columns of a token; the rows' loads of a thread do not depend on one another.  Bound: the rows read.
+// A warp takes runs of 256 columns of a token, eight a lane, and asks for the rows of up to kCbAhead experts at a time before it uses the
+// first.  Bound: the rows read.  (One row after the other, with a 64-bit division for each run: 60 us for 8,192 tokens x 6 of 2,048.)
+constexpr int kCbAhead = 8;
 template <class R, class O, bool WIDE>
 __global__ void __launch_bounds__(kCbThreads) combine_kernel(const CbParams p) {
   mx_dep_launch();
   mx_dep_wait();
-  const int per_row = (p.N + 7) >> 3;
-  const int64_t n = (int64_t)p.T * per_row, step = (int64_t)gridDim.x * kCbThreads;
-  for (int64_t i = (int64_t)blockIdx.x * kCbThreads + threadIdx.x; i < n; i += step) {
-    const int64_t t = i / per_row;
-    const int c = (int)(i - t * per_row) * 8, here = min(8, p.N - c);
-    float acc[8];
+  const int per_row = (p.N + 255) >> 8, lane = threadIdx.x & 31;
+  const int64_t run = ((int64_t)blockIdx.x * kCbThreads + threadIdx.x) >> 5;
+  const int64_t t = (run >> 31) ? run / per_row : (int64_t)((uint32_t)run / (uint32_t)per_row);
+  const int c = (int)(run - t * per_row) * 256 + lane * 8, here = min(8, p.N - c);
+  if (t >= p.T || here <= 0) return;
+  float acc[8];
 #pragma unroll
-    for (int q = 0; q < 8; ++q) acc[q] = 0.0f;
-    if (p.base) {
-      const O* b = static_cast<const O*>(p.base) + t * p.N + c;
-      if constexpr (WIDE) {
-        mx_load8<O, true>(b, acc);
-      } else {
-        for (int q = 0; q < here; ++q) acc[q] = mx_load(b + q);
-      }
-    }
-    for (int j = 0; j < p.k; ++j) {
-      if (p.ids && (unsigned)__ldcg(p.ids + t * p.k + j) >= (unsigned)p.n_experts) continue;
-      const float w = __ldcg(p.weights + t * p.k + j);
-      const R* r = static_cast<const R*>(p.rows) + (t * p.k + j) * p.N + c;
-      float v[8];
-      if constexpr (WIDE) {
-        mx_load8<R, true>(r, v);
-      } else {
-#pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] = q < here ? mx_load(r + q) : 0.0f;
-      }
-#pragma unroll
-      for (int q = 0; q < 8; ++q) acc[q] = fmaf(w, v[q], acc[q]);
-    }
-    O* o = static_cast<O*>(p.out) + t * p.N + c;
+  for (int q = 0; q < 8; ++q) acc[q] = 0.0f;
+  const O* b = static_cast<const O*>(p.base) + t * p.N + c;
+  if (p.base) {
     if constexpr (WIDE) {
-      mx_store8<O, true>(o, acc);
+      mx_load8<O, true>(b, acc);
     } else {
-#pragma unroll
-      for (int q = 0; q < 8; ++q)
-        if (q < here) o[q] = mx_from_float<O>(acc[q]);
+      for (int q = 0; q < here; ++q) acc[q] = mx_load(b + q);
     }
+  }
+  for (int j0 = 0; j0 < p.k; j0 += kCbAhead) {
+    const R* first = static_cast<const R*>(p.rows) + (t * p.k + j0) * p.N + c;
+    float w[kCbAhead];
+    using Raw = typename std::conditional<sizeof(R) == 4, float4, uint2>::type;  // four elements
+    Raw raw[kCbAhead][2];
+    bool in[kCbAhead];
+#pragma unroll
+    for (int j = 0; j < kCbAhead; ++j) {
+      in[j] = j0 + j < p.k;
+      if (in[j] && p.ids) in[j] = (unsigned)__ldcg(p.ids + t * p.k + j0 + j) < (unsigned)p.n_experts;
+      w[j] = in[j] ? __ldcg(p.weights + t * p.k + j0 + j) : 0.0f;
+      if (!in[j]) continue;
+      const R* r = first + (int64_t)j * p.N;
+      if constexpr (!WIDE) {
+        R e[8] = {};
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+          if (q < here) e[q] = mx_from_float<R>(mx_load(r + q));
+        memcpy(raw[j], e, sizeof(e));
+      } else if constexpr (sizeof(R) == 4) {
+        raw[j][0] = __ldcg(reinterpret_cast<const float4*>(r));
+        raw[j][1] = __ldcg(reinterpret_cast<const float4*>(r) + 1);
+      } else {
+        const uint4 v = __ldcg(reinterpret_cast<const uint4*>(r));
+        raw[j][0] = make_uint2(v.x, v.y);
+        raw[j][1] = make_uint2(v.z, v.w);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kCbAhead; ++j) {
+      if (!in[j]) continue;
+      R e[8];
+      memcpy(e, raw[j], sizeof(e));
+#pragma unroll
+      for (int q = 0; q < 8; ++q) acc[q] = fmaf(w[j], mx_to_float<R>(e[q]), acc[q]);
+    }
+  }
+  O* o = static_cast<O*>(p.out) + t * p.N + c;
+  if constexpr (WIDE) {
+    mx_store8<O, true>(o, acc);
+  } else {
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      if (q < here) o[q] = mx_from_float<O>(acc[q]);
   }
 }
 
 template <class R, class O>
 static int combine_as(const CbParams& p, cudaStream_t st) {
   const bool wide = p.N % 8 == 0 && mx_aligned(p.rows, 16) && mx_aligned(p.base, 16) && mx_aligned(p.out, 16);
-  const int64_t blocks = ((int64_t)p.T * ((p.N + 7) / 8) + kCbThreads - 1) / kCbThreads;
-  return mx_launch(wide ? combine_kernel<R, O, true> : combine_kernel<R, O, false>, dim3((unsigned)(blocks < 148 * 64 ? blocks : 148 * 64)), kCbThreads, 0,
-                   st, CbParams(p));
+  const int64_t blocks = ((int64_t)p.T * ((p.N + 255) >> 8) + kCbThreads / 32 - 1) / (kCbThreads / 32);
+  if (blocks > INT32_MAX) return SLICEMOE_E_UNSUPPORTED;
+  return mx_launch(wide ? combine_kernel<R, O, true> : combine_kernel<R, O, false>, dim3((unsigned)blocks), kCbThreads, 0, st, CbParams(p));
 }
 template <class R>
 static int combine_to(const CbParams& p, int out_dtype, cudaStream_t st) {
