@@ -15,73 +15,110 @@ struct CbParams {
 };
 constexpr int kCbThreads = 256;
 
-// A warp takes runs of 256 columns of a token, eight a lane, and asks for the rows of up to kCbAhead experts at a time before it uses the
+// Eight values of a row as pairs of floats.
+__device__ __forceinline__ void cb_pairs(const float4 (&raw)[2], float2 (&v)[4]) {
+  v[0] = make_float2(raw[0].x, raw[0].y), v[1] = make_float2(raw[0].z, raw[0].w), v[2] = make_float2(raw[1].x, raw[1].y), v[3] = make_float2(raw[1].z, raw[1].w);
+}
+template <class R>
+__device__ __forceinline__ void cb_pairs(const uint4 (&raw)[1], float2 (&v)[4]) {
+  const uint32_t w[4] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    R e[2];
+    memcpy(e, &w[i], 4);
+    v[i] = make_float2(mx_to_float<R>(e[0]), mx_to_float<R>(e[1]));
+  }
+}
+// acc += w v, two at a time in one instruction
+__device__ __forceinline__ void cb_fma2(float2& acc, float w, float2 v) {
+  asm("{\n .reg .b64 a, b, c;\n mov.b64 a, {%0, %1};\n mov.b64 b, {%2, %2};\n mov.b64 c, {%3, %4};\n fma.rn.f32x2 a, b, c, a;\n mov.b64 {%0, %1}, a;\n}"
+      : "+f"(acc.x), "+f"(acc.y)
+      : "f"(w), "f"(v.x), "f"(v.y));
+}
+
+// A warp takes a run of 256 columns of a token, eight a lane, and asks for the rows of up to eight (of fp32, four) experts at a time before it uses the
 // first.  Bound: the rows read.  (One row after the other, with a 64-bit division for each run: 60 us for 8,192 tokens x 6 of 2,048.)
-constexpr int kCbAhead = 8;
 template <class R, class O, bool WIDE>
-__global__ void __launch_bounds__(kCbThreads) combine_kernel(const CbParams p) {
+__global__ void __launch_bounds__(kCbThreads, 3) combine_kernel(const CbParams p) {
   mx_dep_launch();
   mx_dep_wait();
   const int per_row = (p.N + 255) >> 8, lane = threadIdx.x & 31;
-  const int64_t run = ((int64_t)blockIdx.x * kCbThreads + threadIdx.x) >> 5;
-  const int64_t t = (run >> 31) ? run / per_row : (int64_t)((uint32_t)run / (uint32_t)per_row);
-  const int c = (int)(run - t * per_row) * 256 + lane * 8, here = min(8, p.N - c);
-  if (t >= p.T || here <= 0) return;
-  float acc[8];
+  const int64_t runs = (int64_t)p.T * per_row, step = (int64_t)gridDim.x * (kCbThreads / 32);
+  constexpr int kCbAhead = sizeof(R) == 4 ? 4 : 8;
+  for (int64_t run = ((int64_t)blockIdx.x * kCbThreads + threadIdx.x) >> 5; run < runs; run += step) {
+    const int64_t t = (run >> 31) ? run / per_row : (int64_t)((uint32_t)run / (uint32_t)per_row);
+    const int c = (int)(run - t * per_row) * 256 + lane * 8, here = min(8, p.N - c);
+    if (here <= 0) continue;
+    const R* row = static_cast<const R*>(p.rows) + t * p.k * p.N + c;
+    const float* weights = p.weights + t * p.k;
+    const int32_t* ids = p.ids ? p.ids + t * p.k : nullptr;
+    float2 acc[4];
+    {
+      float base[8];
 #pragma unroll
-  for (int q = 0; q < 8; ++q) acc[q] = 0.0f;
-  const O* b = static_cast<const O*>(p.base) + t * p.N + c;
-  if (p.base) {
-    if constexpr (WIDE) {
-      mx_load8<O, true>(b, acc);
-    } else {
-      for (int q = 0; q < here; ++q) acc[q] = mx_load(b + q);
+      for (int q = 0; q < 8; ++q) base[q] = 0.0f;
+      if (p.base) {
+        const O* b = static_cast<const O*>(p.base) + t * p.N + c;
+        if constexpr (WIDE) {
+          mx_load8<O, true>(b, base);
+        } else {
+#pragma unroll
+          for (int q = 0; q < 8; ++q)
+            if (q < here) base[q] = mx_load(b + q);
+        }
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) acc[q] = make_float2(base[2 * q], base[2 * q + 1]);
     }
-  }
-  for (int j0 = 0; j0 < p.k; j0 += kCbAhead) {
-    const R* first = static_cast<const R*>(p.rows) + (t * p.k + j0) * p.N + c;
-    float w[kCbAhead];
-    using Raw = typename std::conditional<sizeof(R) == 4, float4, uint2>::type;  // four elements
-    Raw raw[kCbAhead][2];
-    bool in[kCbAhead];
+    if constexpr (WIDE) {
+      constexpr int kPieces = sizeof(R) == 4 ? 2 : 1;
+      using Raw = typename std::conditional<sizeof(R) == 4, float4, uint4>::type;
+      for (int j0 = 0; j0 < p.k; j0 += kCbAhead) {
+        Raw raw[kCbAhead][kPieces];
+        float w[kCbAhead];
+        uint32_t in = 0;
 #pragma unroll
-    for (int j = 0; j < kCbAhead; ++j) {
-      in[j] = j0 + j < p.k;
-      if (in[j] && p.ids) in[j] = (unsigned)__ldcg(p.ids + t * p.k + j0 + j) < (unsigned)p.n_experts;
-      w[j] = in[j] ? __ldcg(p.weights + t * p.k + j0 + j) : 0.0f;
-      if (!in[j]) continue;
-      const R* r = first + (int64_t)j * p.N;
-      if constexpr (!WIDE) {
-        R e[8] = {};
+        for (int j = 0; j < kCbAhead; ++j) {
+          if (j0 + j >= p.k) break;
+          if (!ids || (unsigned)__ldcg(ids + j0 + j) < (unsigned)p.n_experts) {
+            in |= 1u << j;
+            w[j] = __ldcg(weights + j0 + j);
 #pragma unroll
-        for (int q = 0; q < 8; ++q)
-          if (q < here) e[q] = mx_from_float<R>(mx_load(r + q));
-        memcpy(raw[j], e, sizeof(e));
-      } else if constexpr (sizeof(R) == 4) {
-        raw[j][0] = __ldcg(reinterpret_cast<const float4*>(r));
-        raw[j][1] = __ldcg(reinterpret_cast<const float4*>(r) + 1);
-      } else {
-        const uint4 v = __ldcg(reinterpret_cast<const uint4*>(r));
-        raw[j][0] = make_uint2(v.x, v.y);
-        raw[j][1] = make_uint2(v.z, v.w);
+            for (int h = 0; h < kPieces; ++h) raw[j][h] = __ldcg(reinterpret_cast<const Raw*>(row) + h);
+          }
+          row += p.N;
+        }
+#pragma unroll
+        for (int j = 0; j < kCbAhead; ++j) {
+          if (j0 + j >= p.k) break;
+          if (!((in >> j) & 1u)) continue;
+          float2 v[4];
+          if constexpr (sizeof(R) == 4) cb_pairs(raw[j], v);
+          else cb_pairs<R>(raw[j], v);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) cb_fma2(acc[q], w[j], v[q]);
+        }
+      }
+    } else {
+      for (int j = 0; j < p.k; ++j, row += p.N) {
+        if (ids && (unsigned)__ldcg(ids + j) >= (unsigned)p.n_experts) continue;
+        const float w = __ldcg(weights + j);
+        float v[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] = q < here ? mx_load(row + q) : 0.0f;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) cb_fma2(acc[q], w, make_float2(v[2 * q], v[2 * q + 1]));
       }
     }
+    const float y[8] = {acc[0].x, acc[0].y, acc[1].x, acc[1].y, acc[2].x, acc[2].y, acc[3].x, acc[3].y};
+    O* o = static_cast<O*>(p.out) + t * p.N + c;
+    if constexpr (WIDE) {
+      mx_store8<O, true>(o, y);
+    } else {
 #pragma unroll
-    for (int j = 0; j < kCbAhead; ++j) {
-      if (!in[j]) continue;
-      R e[8];
-      memcpy(e, raw[j], sizeof(e));
-#pragma unroll
-      for (int q = 0; q < 8; ++q) acc[q] = fmaf(w[j], mx_to_float<R>(e[q]), acc[q]);
+      for (int q = 0; q < 8; ++q)
+        if (q < here) o[q] = mx_from_float<O>(y[q]);
     }
-  }
-  O* o = static_cast<O*>(p.out) + t * p.N + c;
-  if constexpr (WIDE) {
-    mx_store8<O, true>(o, acc);
-  } else {
-#pragma unroll
-    for (int q = 0; q < 8; ++q)
-      if (q < here) o[q] = mx_from_float<O>(acc[q]);
   }
 }
 
@@ -89,8 +126,8 @@ template <class R, class O>
 static int combine_as(const CbParams& p, cudaStream_t st) {
   const bool wide = p.N % 8 == 0 && mx_aligned(p.rows, 16) && mx_aligned(p.base, 16) && mx_aligned(p.out, 16);
   const int64_t blocks = ((int64_t)p.T * ((p.N + 255) >> 8) + kCbThreads / 32 - 1) / (kCbThreads / 32);
-  if (blocks > INT32_MAX) return SLICEMOE_E_UNSUPPORTED;
-  return mx_launch(wide ? combine_kernel<R, O, true> : combine_kernel<R, O, false>, dim3((unsigned)blocks), kCbThreads, 0, st, CbParams(p));
+  return mx_launch(wide ? combine_kernel<R, O, true> : combine_kernel<R, O, false>, dim3((unsigned)(blocks < (1 << 20) ? blocks : 1 << 20)), kCbThreads, 0, st,
+                   CbParams(p));
 }
 template <class R>
 static int combine_to(const CbParams& p, int out_dtype, cudaStream_t st) {

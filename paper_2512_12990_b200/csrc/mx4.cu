@@ -26,44 +26,102 @@ __device__ __forceinline__ void mx_runs(int64_t first, int64_t rows, int per_row
   }
 }
 
+// Eight values as they are loaded; the bits of the largest magnitude among them, as fp32; the values.
+template <class T>
+struct MxRaw;
+template <>
+struct MxRaw<float> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float* p) { a = __ldcg(reinterpret_cast<const float4*>(p)), b = __ldcg(reinterpret_cast<const float4*>(p) + 1); }
+  __device__ __forceinline__ void one_by_one(const float* p) { a = make_float4(__ldcg(p), __ldcg(p + 1), __ldcg(p + 2), __ldcg(p + 3)), b = make_float4(__ldcg(p + 4), __ldcg(p + 5), __ldcg(p + 6), __ldcg(p + 7)); }
+  __device__ __forceinline__ void values(float (&v)[8]) const { v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w; }
+  __device__ __forceinline__ uint32_t largest() const {
+    float v[8];
+    values(v);
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(v[j]) & 0x7fffffffu);
+    return m;
+  }
+};
+template <class T>
+struct MxRaw {  // 16 bits: two to a word
+  uint4 a;
+  __device__ __forceinline__ void load(const T* p) { a = __ldcg(reinterpret_cast<const uint4*>(p)); }
+  __device__ __forceinline__ void one_by_one(const T* p) {
+    uint32_t h[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) h[j] = __ldcg(reinterpret_cast<const unsigned short*>(p) + j);
+    a = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+  }
+  __device__ __forceinline__ void values(float (&v)[8]) const {
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      T e[2];
+      memcpy(e, &w[i], 4);
+      v[2 * i] = mx_to_float<T>(e[0]), v[2 * i + 1] = mx_to_float<T>(e[1]);
+    }
+  }
+  __device__ __forceinline__ uint32_t largest() const {  // magnitudes order like their bits, infinities and NaN above all
+    constexpr uint32_t kMag = 0x7fff7fffu;
+    const uint32_t m = __vmaxu2(__vmaxu2(a.x & kMag, a.y & kMag), __vmaxu2(a.z & kMag, a.w & kMag));
+    const unsigned short h = (unsigned short)max(m >> 16, m & 0xffffu);
+    T e;
+    memcpy(&e, &h, 2);
+    return __float_as_uint(mx_to_float<T>(e)) & 0x7fffffffu;
+  }
+};
+
 // Four lanes hold a block of 32 values, eight each: the largest magnitude by two exchanges, then each lane writes the four bytes
-// of its eight codes (a warp's stores are 128 consecutive bytes) and the first the scale.  Bound: the values read.
-template <class T, bool WIDE>
-__global__ void __launch_bounds__(kMxThreads) mx_quantize_kernel(const T* __restrict__ x, int rows, int K, int64_t ld,
-                                                                 uint8_t* __restrict__ codes, uint8_t* __restrict__ scale) {
+// of its eight codes (a warp's stores are 128 consecutive bytes) and the first the scale.  LINEAR: the rows are one behind the other
+// and whole runs, so that a place is a shift of a counter.  Bound: the values read.
+template <class T, bool WIDE, bool LINEAR>
+__global__ void __launch_bounds__(kMxThreads) mx_quantize_kernel(const T* __restrict__ x, int rows, int K, int64_t ld, uint8_t* __restrict__ codes,
+                                                                 uint8_t* __restrict__ scale) {
   mx_dep_launch();
   mx_dep_wait();
   const int pitch = mx_pitch(K), blocks = K / kMxBlock, per_row = (K + 255) >> 8, lane = threadIdx.x & 31;
-  const int64_t warp = ((int64_t)blockIdx.x * kMxThreads + threadIdx.x) >> 5;
-  MxRun run[kMxAhead];
-  mx_runs(warp * kMxAhead, rows, per_row, K, lane, run);
-  float v[kMxAhead][8];
+  const int64_t runs = (int64_t)rows * per_row, step = (int64_t)gridDim.x * (kMxThreads / 32) * kMxAhead;
+  for (int64_t first = (((int64_t)blockIdx.x * kMxThreads + threadIdx.x) >> 5) * kMxAhead; first < runs; first += step) {
+    MxRun run[kMxAhead];
+    if constexpr (!LINEAR) mx_runs(first, rows, per_row, K, lane, run);
+    const int64_t at = first * 256 + lane * 8;
+    MxRaw<T> raw[kMxAhead];
 #pragma unroll
-  for (int i = 0; i < kMxAhead; ++i) {
-    if (run[i].live) mx_load8<T, WIDE>(x + run[i].row * ld + run[i].c, v[i]);
-  }
-#pragma unroll
-  for (int i = 0; i < kMxAhead; ++i) {
-    uint32_t m = 0;
-    if (run[i].live) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(v[i][j]) & 0x7fffffffu);
+    for (int i = 0; i < kMxAhead; ++i) {
+      if constexpr (LINEAR) {
+        if (first + i < runs) raw[i].load(x + at + 256 * i);
+      } else if (run[i].live) {
+        const T* src = x + run[i].row * ld + run[i].c;
+        if constexpr (WIDE) raw[i].load(src);
+        else raw[i].one_by_one(src);
+      }
     }
-    m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-    m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-    if (!run[i].live) continue;
-    const uint32_t b = mx_scale_byte(m);
-    if (b == 255u) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] = 0.0f;
-    }
-    *reinterpret_cast<uint32_t*>(codes + run[i].row * (K >> 1) + (run[i].c >> 1)) = mx_encode8(v[i], mx_inverse(b));
-    if ((lane & 3) == 0) {
-      const int kb = run[i].c / kMxBlock;
-      uint8_t* s = scale + run[i].row * pitch;
-      s[kb] = (uint8_t)b;
-      if (kb == blocks - 1)
-        for (int p = blocks; p < pitch; ++p) s[p] = 0;
+    for (int i = 0; i < kMxAhead; ++i) {
+      const bool live = LINEAR ? first + i < runs : run[i].live;
+      uint32_t m = live ? raw[i].largest() : 0u;
+      m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+      m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+      if (!live) continue;
+      const uint32_t b = mx_scale_byte(m);
+      float v[8];
+      raw[i].values(v);
+      const uint32_t w = b == 255u ? 0u : mx_encode8(v, mx_inverse(b));
+      if constexpr (LINEAR) {
+        *reinterpret_cast<uint32_t*>(codes + (at >> 1) + 128 * i) = w;
+        if ((lane & 3) == 0) scale[(at >> 5) + 8 * i] = (uint8_t)b;
+      } else {
+        *reinterpret_cast<uint32_t*>(codes + run[i].row * (K >> 1) + (run[i].c >> 1)) = w;
+        if ((lane & 3) == 0) {
+          const int kb = run[i].c / kMxBlock;
+          uint8_t* s = scale + run[i].row * pitch;
+          s[kb] = (uint8_t)b;
+          if (kb == blocks - 1)
+            for (int p = blocks; p < pitch; ++p) s[p] = 0;
+        }
+      }
     }
   }
 }
@@ -175,8 +233,8 @@ static int quantize_as(const void* x, int rows, int K, int64_t ld, uint8_t* code
   const bool wide = mx_aligned(x, 16) && (ld * sizeof(T)) % 16 == 0;
   const unsigned blocks = mx_run_blocks(rows, K);
   if (!blocks) return SLICEMOE_E_UNSUPPORTED;
-  return mx_launch(wide ? mx_quantize_kernel<T, true> : mx_quantize_kernel<T, false>, dim3(blocks), kMxThreads, 0, st,
-                   static_cast<const T*>(x), rows, K, ld, codes, scale);
+  const auto kernel = wide && ld == K && K % 256 == 0 ? mx_quantize_kernel<T, true, true> : wide ? mx_quantize_kernel<T, true, false> : mx_quantize_kernel<T, false, false>;
+  return mx_launch(kernel, dim3(blocks < 148 * 8 ? blocks : 148 * 8), kMxThreads, 0, st, static_cast<const T*>(x), rows, K, ld, codes, scale);
 }
 template <class T>
 static int dequantize_as(const uint8_t* codes, const uint8_t* scale, int rows, int K, void* out, int64_t ld, cudaStream_t st) {
