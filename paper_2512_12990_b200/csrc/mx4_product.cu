@@ -729,52 +729,66 @@ __global__ void __launch_bounds__(kMpThreads, 1) mp_product_kernel(const MpParam
         groups &= groups - 1u;
         uint32_t r[16];
         mp_ld16(d + c0, r);
-        const int4* pairs = reinterpret_cast<const int4*>(&s->pair[slot][c0]);
-        int pr[16];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int4 v = pairs[i];
-          pr[4 * i] = v.x, pr[4 * i + 1] = v.y, pr[4 * i + 2] = v.z, pr[4 * i + 3] = v.w;
-        }
+        const int* pairs = &s->pair[slot][c0];
+        // Results of 16 bits leave as pairs of columns: two tokens' values in a word, half of the words exchanged with the neighbouring
+        // lane, and each lane has both columns of half of the tokens.  Exchanges and stores go the way that the products' operands
+        // take out of shared memory, and are what a long prompt's drain waits for: with an exchange for every word it took 5,700
+        // clocks an item of 224 tokens, more than the products.
+        const bool odd = lane & 1;
         if constexpr (GATED) {
           // lanes 0 to 15 hold gate, 16 to 31 up of the same columns of the result: of two tokens, the lower lanes take the first
-          const bool hi = lane & 16, odd = lane & 1;
+          const bool hi = lane & 16;
           const int col = rb * 64 + quarter * 16 + (lane & 15);
-          float h[8];
+          float h[8];  // of tokens 2 i + hi
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const float v0 = __uint_as_float(r[2 * i]), v1 = __uint_as_float(r[2 * i + 1]);
             const float got = __shfl_xor_sync(0xffffffffu, hi ? v0 : v1, 16);
             h[i] = mp_gated(hi ? got : v0, hi ? v1 : got);
           }
-          if (sizeof(O) == 2 && (p.N & 1) == 0) {  // two columns of one token to a lane
+          if (sizeof(O) == 2 && (p.N & 1) == 0) {
+            uint32_t w[4], got[2];
 #pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-              const float got = __shfl_xor_sync(0xffffffffu, odd ? h[i] : h[i + 1], 1);
-              const int lo = odd ? pr[2 * i + 2] : pr[2 * i], up = odd ? pr[2 * i + 3] : pr[2 * i + 1], pair = hi ? up : lo;
-              if (pair >= 0 && col < p.N)
-                *reinterpret_cast<uint32_t*>(out + (size_t)pair * p.N + (col & ~1)) = mp_pack2<O>(odd ? got : h[i], odd ? h[i + 1] : got);
+            for (int i = 0; i < 4; ++i) w[i] = mp_pack2<O>(h[2 * i], h[2 * i + 1]);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) got[i] = __shfl_xor_sync(0xffffffffu, odd ? w[i] : w[2 + i], 1);
+            const int4 a = *reinterpret_cast<const int4*>(pairs + (odd ? 8 : 0)), b = *reinterpret_cast<const int4*>(pairs + (odd ? 12 : 4));
+            const int pr[4] = {hi ? a.y : a.x, hi ? a.w : a.z, hi ? b.y : b.x, hi ? b.w : b.z};
+            if (col < p.N) {
+              O* at = out + (col & ~1);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const uint32_t mine = odd ? w[2 + (i >> 1)] : w[i >> 1], first = odd ? got[i >> 1] : mine, second = odd ? mine : got[i >> 1];
+                if (pr[i] >= 0) *reinterpret_cast<uint32_t*>(at + (size_t)pr[i] * p.N) = __byte_perm(first, second, i & 1 ? 0x7632 : 0x5410);
+              }
             }
-          } else {
+          } else if (col < p.N) {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-              if (const int pair = hi ? pr[2 * i + 1] : pr[2 * i]; pair >= 0 && col < p.N) out[(size_t)pair * p.N + col] = mx_from_float<O>(h[i]);
+              if (const int pair = pairs[2 * i + (hi ? 1 : 0)]; pair >= 0) out[(size_t)pair * p.N + col] = mx_from_float<O>(h[i]);
           }
         } else {
           const int col = rb * kMxRows + quarter * 32 + lane;
-          if (sizeof(O) == 2 && (p.N & 1) == 0) {  // two columns of one token to a lane
-            const bool hi = lane & 1;
+          if (sizeof(O) == 2 && (p.N & 1) == 0) {
+            uint32_t w[8], got[4];
 #pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-              const float v0 = __uint_as_float(r[i]), v1 = __uint_as_float(r[i + 1]);
-              const float got = __shfl_xor_sync(0xffffffffu, hi ? v0 : v1, 1);
-              if (const int pair = hi ? pr[i + 1] : pr[i]; pair >= 0 && col < p.N)
-                *reinterpret_cast<uint32_t*>(out + (size_t)pair * p.N + (col & ~1)) = mp_pack2<O>(hi ? got : v0, hi ? v1 : got);
+            for (int i = 0; i < 8; ++i) w[i] = mp_pack2<O>(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) got[i] = __shfl_xor_sync(0xffffffffu, odd ? w[i] : w[4 + i], 1);
+            const int4 a = *reinterpret_cast<const int4*>(pairs + (odd ? 8 : 0)), b = *reinterpret_cast<const int4*>(pairs + (odd ? 12 : 4));
+            const int pr[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+            if (col < p.N) {
+              O* at = out + (col & ~1);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const uint32_t mine = odd ? w[4 + (i >> 1)] : w[i >> 1], first = odd ? got[i >> 1] : mine, second = odd ? mine : got[i >> 1];
+                if (pr[i] >= 0) *reinterpret_cast<uint32_t*>(at + (size_t)pr[i] * p.N) = __byte_perm(first, second, i & 1 ? 0x7632 : 0x5410);
+              }
             }
-          } else {
+          } else if (col < p.N) {
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-              if (pr[i] >= 0 && col < p.N) out[(size_t)pr[i] * p.N + col] = mx_from_float<O>(__uint_as_float(r[i]));
+              if (const int pair = pairs[i]; pair >= 0) out[(size_t)pair * p.N + col] = mx_from_float<O>(__uint_as_float(r[i]));
           }
         }
       }
