@@ -268,7 +268,7 @@ struct MpItem {
 };
 struct __align__(16) MpSmem {
   unsigned long long full[kMpMaxStages], free_[kMpMaxStages];
-  unsigned long long acc_full[2], acc_free[2], item_full[kMpSlots], item_free[kMpSlots], resident, drain;
+  unsigned long long acc_full[2], acc_free[2], item_known[kMpSlots], item_full[kMpSlots], item_free[kMpSlots], resident, drain;
   uint32_t tmem;
   int pad0;
   int dead, pad1;
@@ -401,19 +401,14 @@ __global__ void __launch_bounds__(kMpThreads, 1) mp_product_kernel(const MpParam
   } else if (warp >= kMpFirstDrain && warp < kMpFirstDrain + 2) {
     // one barrier to a thread: they lie one behind the other in the order of MpSmem
     const int i = tid - 32 * kMpFirstDrain;
-    constexpr int kRing = 2 * kMpMaxStages, kAll = kRing + 4 + 2 * kMpSlots + 2;
+    constexpr int kRing = 2 * kMpMaxStages, kAll = kRing + 4 + 3 * kMpSlots + 2;
     static_assert(kAll <= 64 && offsetof(MpSmem, drain) == 8 * (kAll - 1), "barriers");
     int arrivals = 1;
     if (i >= kRing + 2 && i < kRing + 4) arrivals = kMpDrainWarps;
-    if (i >= kRing + 4 + kMpSlots && i < kRing + 4 + 2 * kMpSlots) arrivals = 2 + kMpDrainWarps;
+    if (i >= kRing + 4 + 2 * kMpSlots && i < kRing + 4 + 3 * kMpSlots) arrivals = 2 + kMpDrainWarps;
     if (i == kAll - 2) arrivals = kMpDrainWarps + 1;
     if (i < kAll) mbar_init(smem_u32(&s->full[0] + i), arrivals);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  } else if (warp >= kMpFirstDrain + 4 && warp < kMpFirstDrain + 8 && p.E <= kMpTable) {
-    // the table does not change between launches: it is read while the kernel before is still at work
-    constexpr int kWords = sizeof(slicemoe_mx4_mat) / 8;
-    for (int i = tid - 32 * (kMpFirstDrain + 4); i < p.E * kWords; i += 128)
-      reinterpret_cast<unsigned long long*>(s->mats)[i] = __ldg(reinterpret_cast<const unsigned long long*>(p.mats) + i);
   }
   const int pairs = p.T * p.k;
   if (!PLACED && pairs > 32)
@@ -450,6 +445,19 @@ __global__ void __launch_bounds__(kMpThreads, 1) mp_product_kernel(const MpParam
     int at = blockIdx.x / p.row_blocks, rest = blockIdx.x - at * p.row_blocks;  // an item's place among the tiles
     const int at_step = gridDim.x / p.row_blocks, rest_step = gridDim.x - at_step * p.row_blocks;
     int total_tiles = 0;
+    if (p.E <= kMpTable) {
+      // the table does not change between launches: it is asked for while the kernel before is still at work
+      constexpr int kWords = sizeof(slicemoe_mx4_mat) / 8, kAhead = 8;
+      for (int i0 = lane; i0 < p.E * kWords; i0 += 32 * kAhead) {
+        unsigned long long w[kAhead];
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a)
+          if (i0 + 32 * a < p.E * kWords) w[a] = __ldg(reinterpret_cast<const unsigned long long*>(p.mats) + i0 + 32 * a);
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a)
+          if (i0 + 32 * a < p.E * kWords) reinterpret_cast<unsigned long long*>(s->mats)[i0 + 32 * a] = w[a];
+      }
+    }
     mx_dep_wait();
     if constexpr (PLACED) {
       for (int e = lane; e <= p.E; e += 32) {
@@ -495,9 +503,11 @@ __global__ void __launch_bounds__(kMpThreads, 1) mp_product_kernel(const MpParam
       if (rest >= p.row_blocks) rest -= p.row_blocks, ++at;
       if (!mp_wait(&s->item_free[slot], turn ^ 1u, s, status)) break;
       if (at >= total_tiles) {
-        if (lane == 0) s->item[slot].n = -1;
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&s->item_full[slot]));
+        if (lane == 0) {
+          s->item[slot].n = -1;
+          mbar_arrive(smem_u32(&s->item_known[slot]));
+          mbar_arrive(smem_u32(&s->item_full[slot]));
+        }
         break;
       }
       int e, key = 0;
@@ -513,27 +523,39 @@ __global__ void __launch_bounds__(kMpThreads, 1) mp_product_kernel(const MpParam
         if (lane == 0) atomicOr(status, (unsigned)SLICEMOE_STATUS_BAD_EXPERT_ID);
         continue;
       }
+      // first what the weights and the products need, then where the results go
       MpItem* item = &s->item[slot];
-      int rb = rest;
+      int rb = rest, list_at = 0, n = 0, n16 = p.tile;
       if constexpr (PLACED) {
         // of an expert's items a row block's tiles come one after the other: its weights are in L2 for all but the first
         const int first = s->first[e], count = s->first[e + 1] - first, e_tile = s->tiles[e];
         const MpTiles tt = count <= p.tile ? MpTiles{1, (count + 15) & ~15} : mp_tiles(count, p.tile);
         const int local = (at - e_tile) * p.row_blocks + rest;
         rb = tt.n == 1 ? local : local / tt.n;
-        const int t = local - rb * tt.n, r0 = t * tt.each, n = min(tt.each, count - r0), n16 = (n + 15) & ~15;
-        for (int i = lane; i < n16; i += 32) s->pair[slot][i] = i < n ? __ldcg(p.list + first + r0 + i) : -1;
+        const int t = local - rb * tt.n, r0 = t * tt.each;
+        n = min(tt.each, count - r0), n16 = (n + 15) & ~15, list_at = first + r0;
         if (lane == 0) {
           item->t_codes = p.t_codes + (size_t)(s->padded[e] + r0) * steps * kMpRowBytes;
           item->t_scale = p.t_scale + (size_t)(e_tile + t) * atoms * halves * kMxAtomBytes;
-          item->n = n16;
           item->rows = tt.each;
-          item->groups = (1u << (n16 >> 4)) - 1u;
         }
+      } else if (lane == 0) {
+        item->rows = p.tile;
+      }
+      if (lane == 0) {
+        item->n = n16;
+        item->codes = m.codes + (size_t)rb * chunks * kMxChunkBytes;
+        item->scale = m.scale + (size_t)rb * atoms * kMxAtomBytes;
+        item->rb = rb;
+        mbar_arrive(smem_u32(&s->item_known[slot]));
+      }
+      uint32_t groups = (1u << (n16 >> 4)) - 1u;
+      if constexpr (PLACED) {
+        for (int i = lane; i < n16; i += 32) s->pair[slot][i] = i < n ? __ldcg(p.list + list_at + i) : -1;
       } else {
         for (int i = lane; i < p.tile; i += 32) s->pair[slot][i] = -1;
         __syncwarp();
-        uint32_t groups = 0;
+        groups = 0;
         for (int i = lane; i < pairs; i += 32)
           if (s->key[i] == key) {
             const int row = p.x_per_pair ? i : (int)__umulhi((uint32_t)i, p.k_inverse);
@@ -541,16 +563,8 @@ __global__ void __launch_bounds__(kMpThreads, 1) mp_product_kernel(const MpParam
             groups |= 1u << (row >> 4);
           }
         groups = __reduce_or_sync(0xffffffffu, groups);
-        if (lane == 0) {
-          item->n = item->rows = p.tile;
-          item->groups = groups;
-        }
       }
-      if (lane == 0) {
-        item->codes = m.codes + (size_t)rb * chunks * kMxChunkBytes;
-        item->scale = m.scale + (size_t)rb * atoms * kMxAtomBytes;
-        item->rb = rb;
-      }
+      if (lane == 0) item->groups = groups;
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&s->item_full[slot]));
       if (++slot == kMpSlots) slot = 0, turn ^= 1u;
@@ -567,7 +581,7 @@ __global__ void __launch_bounds__(kMpThreads, 1) mp_product_kernel(const MpParam
         asm volatile("fence.proxy.async;" ::: "memory");  // the tiles were written by ordinary stores
       }
       bool ok = true;
-      while (ok && (ok = mbar_wait(smem_u32(&s->item_full[slot]), turn, &s->dead, status))) {
+      while (ok && (ok = mbar_wait(smem_u32(&s->item_known[slot]), turn, &s->dead, status))) {
         const MpItem item = s->item[slot];
         if (item.n < 0) break;
         const uint32_t bytes = PLACED ? mp_step_bytes(item.rows, halves) : kMpABytes + kMpAScaleBytes, t_step = item.rows * kMpRowBytes;
@@ -623,7 +637,7 @@ __global__ void __launch_bounds__(kMpThreads, 1) mp_product_kernel(const MpParam
     if (mp_elect()) {
       uint32_t slot = 0, turn = 0, st = 0, ph = 0, acc = 0, acc_ph = 0, flip = 0, head = 0;
       bool ok = PLACED || mbar_wait(smem_u32(&s->resident), 0, &s->dead, status);
-      while (ok && (ok = mbar_wait(smem_u32(&s->item_full[slot]), turn, &s->dead, status))) {
+      while (ok && (ok = mbar_wait(smem_u32(&s->item_known[slot]), turn, &s->dead, status))) {
         const int n = s->item[slot].n, rows = s->item[slot].rows;
         if (n < 0) break;
         const uint32_t idesc = mp_idesc(n), d = tmem + acc * kMpTile;
