@@ -248,7 +248,7 @@ __global__ void __launch_bounds__(kMpPlaceThreads, 4) mp_place_kernel(const MpPl
 }
 
 // ---- the product ----------------------------------------------------------------------------------------------------
-constexpr int kMpWeightWarp = 0, kMpMmaWarp = 1, kMpPlanWarp = 2, kMpFirstDrain = 4, kMpDrainWarps = 8;  // warp 3 helps to lay out resident rows
+constexpr int kMpWeightWarp = 0, kMpMmaWarp = 1, kMpPlanWarp = 2, kMpTileWarp = 3, kMpFirstDrain = 4, kMpDrainWarps = 8;  // the fourth brings placed tiles, or helps to lay out resident rows
 constexpr int kMpThreads = 32 * (kMpFirstDrain + kMpDrainWarps);
 constexpr int kMpTable = 128;                // table entries that a CTA keeps in shared memory
 constexpr int kMpSlots = 4, kMpMaxStages = 12;
@@ -279,7 +279,7 @@ struct __align__(16) MpSmem {
   int first[kMpMaxExperts + 1];  // rows before an expert
   int tiles[kMpMaxExperts + 1];  // tiles before it
   int padded[kMpMaxExperts];     // rows of the tiles before it
-  uint32_t place[kMpMaxStages];  // where the steps under way begin
+  uint32_t place[2][kMpMaxStages];  // where the steps under way begin, as either filler knows it
   int key[kMpFew], tile[kMpFew]; // of a pair, and of a tile, where the CTA plans for itself: expert, and how often the token named it before << 16
 };
 static_assert(offsetof(MpSmem, pair) % 16 == 0 && kMpTile % 4 == 0 && offsetof(MpSmem, mats) % 8 == 0, "alignment");
@@ -403,9 +403,9 @@ __global__ void __launch_bounds__(kMpThreads, 1) mp_product_kernel(const MpParam
     const int i = tid - 32 * kMpFirstDrain;
     constexpr int kRing = 2 * kMpMaxStages, kAll = kRing + 4 + 3 * kMpSlots + 2;
     static_assert(kAll <= 64 && offsetof(MpSmem, drain) == 8 * (kAll - 1), "barriers");
-    int arrivals = 1;
+    int arrivals = i < kMpMaxStages && PLACED ? 2 : 1;
     if (i >= kRing + 2 && i < kRing + 4) arrivals = kMpDrainWarps;
-    if (i >= kRing + 4 + 2 * kMpSlots && i < kRing + 4 + 3 * kMpSlots) arrivals = 2 + kMpDrainWarps;
+    if (i >= kRing + 4 + 2 * kMpSlots && i < kRing + 4 + 3 * kMpSlots) arrivals = (PLACED ? 3 : 2) + kMpDrainWarps;
     if (i == kAll - 2) arrivals = kMpDrainWarps + 1;
     if (i < kAll) mbar_init(smem_u32(&s->full[0] + i), arrivals);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -569,9 +569,11 @@ __global__ void __launch_bounds__(kMpThreads, 1) mp_product_kernel(const MpParam
       if (lane == 0) mbar_arrive(smem_u32(&s->item_full[slot]));
       if (++slot == kMpSlots) slot = 0, turn ^= 1u;
     }
-  } else if (warp == kMpWeightWarp) {
-    // ---- weights, and placed tiles.  One thread, and the compiler knows it: addresses stay on the uniform datapath ----
+  } else if (warp == kMpWeightWarp || (PLACED && warp == kMpTileWarp)) {
+    // ---- weights by one warp, placed tiles by another.  One thread, and the compiler knows it: addresses stay on the uniform datapath ----
+    const bool tiles = PLACED && warp == kMpTileWarp;
     if (mp_elect()) {
+      uint32_t* place = s->place[tiles ? 1 : 0];
       uint32_t slot = 0, turn = 0, st = 0, head = 0;
       uint32_t live = 0, old = 0, old_ph = 0;  // steps not known to be consumed, the oldest one's barrier
       uint32_t filled = 0;
@@ -591,7 +593,7 @@ __global__ void __launch_bounds__(kMpThreads, 1) mp_product_kernel(const MpParam
             at = head + bytes <= (uint32_t)p.ring ? head : 0;
             if (live == 0) break;
             // what is live lies in [tail, head), or in [tail, ...) and [0, head) where it has started again at 0
-            const uint32_t tail = s->place[old];
+            const uint32_t tail = place[old];
             const bool room = head > tail ? at == head || bytes <= tail : at == head && head + bytes <= tail;
             if (room && live < (uint32_t)p.stages) break;
             if (!(ok = mbar_wait(smem_u32(&s->free_[old]), old_ph, &s->dead, status))) break;
@@ -600,19 +602,20 @@ __global__ void __launch_bounds__(kMpThreads, 1) mp_product_kernel(const MpParam
           }
           if (!ok) break;
           head = at + bytes;
-          s->place[st] = at;
+          place[st] = at;
           ++live;
           if (bring) {
             const int c = min(kMpStepChunks, chunks - i * kMpStepChunks), a = (c + 1) >> 1;
             const uint32_t dst = ring + at, bar = smem_u32(&s->full[st]);
-            const uint32_t t_bytes = PLACED ? t_step : 0, ts_bytes = PLACED ? a * halves * kMxAtomBytes : 0;
-            mbar_arrive_expect_tx(bar, c * kMxChunkBytes + a * kMxAtomBytes + t_bytes + ts_bytes);
-            mp_bulk(dst, item.codes + (size_t)i * kMpABytes, c * kMxChunkBytes, bar);
-            mp_bulk(dst + kMpABytes, item.scale + (size_t)i * kMpAScaleBytes, a * kMxAtomBytes, bar);
-            if constexpr (PLACED) {
-              const uint32_t t_dst = dst + kMpABytes + kMpAScaleBytes;
-              mp_bulk(t_dst, item.t_codes + (size_t)i * t_step, t_bytes, bar);
-              mp_bulk(t_dst + t_step, item.t_scale + (size_t)i * halves * kMpAScaleBytes, ts_bytes, bar);
+            if (tiles) {
+              const uint32_t t_dst = dst + kMpABytes + kMpAScaleBytes, s_bytes = a * halves * kMxAtomBytes;
+              mbar_arrive_expect_tx(bar, t_step + s_bytes);
+              mp_bulk(t_dst, item.t_codes + (size_t)i * t_step, t_step, bar);
+              mp_bulk(t_dst + t_step, item.t_scale + (size_t)i * halves * kMpAScaleBytes, s_bytes, bar);
+            } else {
+              mbar_arrive_expect_tx(bar, c * kMxChunkBytes + a * kMxAtomBytes);
+              mp_bulk(dst, item.codes + (size_t)i * kMpABytes, c * kMxChunkBytes, bar);
+              mp_bulk(dst + kMpABytes, item.scale + (size_t)i * kMpAScaleBytes, a * kMxAtomBytes, bar);
             }
             ++filled;
           }
