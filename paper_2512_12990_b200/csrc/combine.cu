@@ -36,7 +36,8 @@ __device__ __forceinline__ void cb_fma2(float2& acc, float w, float2 v) {
       : "f"(w), "f"(v.x), "f"(v.y));
 }
 
-// A warp takes a run of 256 columns of a token, eight a lane, and asks for the rows of up to eight (of fp32, four) experts at a time before it uses the
+// A warp takes a run of 256 columns of a token, eight a lane (next to one another where rows begin on 16 bytes, else 32 apart, so that a
+// warp's loads are whole lines either way), and asks for the rows of up to eight (of fp32, four) experts at a time before it uses the
 // first.  Bound: the rows read.  (One row after the other, with a 64-bit division for each run: 60 us for 8,192 tokens x 6 of 2,048.)
 template <class R, class O, bool WIDE>
 __global__ void __launch_bounds__(kCbThreads, 3) combine_kernel(const CbParams p) {
@@ -47,8 +48,9 @@ __global__ void __launch_bounds__(kCbThreads, 3) combine_kernel(const CbParams p
   constexpr int kCbAhead = sizeof(R) == 4 ? 4 : 8;
   for (int64_t run = ((int64_t)blockIdx.x * kCbThreads + threadIdx.x) >> 5; run < runs; run += step) {
     const int64_t t = (run >> 31) ? run / per_row : (int64_t)((uint32_t)run / (uint32_t)per_row);
-    const int c = (int)(run - t * per_row) * 256 + lane * 8, here = min(8, p.N - c);
-    if (here <= 0) continue;
+    const int c0 = (int)(run - t * per_row) * 256, c = c0 + (WIDE ? lane * 8 : lane);
+    if (c >= p.N) continue;
+    const int here = WIDE ? 8 : (p.N - c + 31) >> 5;  // of the lane's columns
     const R* row = static_cast<const R*>(p.rows) + t * p.k * p.N + c;
     const float* weights = p.weights + t * p.k;
     const int32_t* ids = p.ids ? p.ids + t * p.k : nullptr;
@@ -64,7 +66,7 @@ __global__ void __launch_bounds__(kCbThreads, 3) combine_kernel(const CbParams p
         } else {
 #pragma unroll
           for (int q = 0; q < 8; ++q)
-            if (q < here) base[q] = mx_load(b + q);
+            if (q < here) base[q] = mx_load(b + 32 * q);
         }
       }
 #pragma unroll
@@ -100,14 +102,20 @@ __global__ void __launch_bounds__(kCbThreads, 3) combine_kernel(const CbParams p
         }
       }
     } else {
-      for (int j = 0; j < p.k; ++j, row += p.N) {
-        if (ids && (unsigned)__ldcg(ids + j) >= (unsigned)p.n_experts) continue;
-        const float w = __ldcg(weights + j);
-        float v[8];
+      // two rows at a time
+      for (int j = 0; j < p.k; j += 2, row += 2 * p.N) {
+        float v[2][8], w[2];
 #pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] = q < here ? mx_load(row + q) : 0.0f;
+        for (int h = 0; h < 2; ++h) {
+          const bool in = j + h < p.k && (!ids || (unsigned)__ldcg(ids + j + h) < (unsigned)p.n_experts);
+          w[h] = in ? __ldcg(weights + j + h) : 0.0f;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) cb_fma2(acc[q], w, make_float2(v[2 * q], v[2 * q + 1]));
+          for (int q = 0; q < 8; ++q) v[h][q] = in && q < here ? mx_load(row + (int64_t)h * p.N + 32 * q) : 0.0f;
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) cb_fma2(acc[q], w[h], make_float2(v[h][2 * q], v[h][2 * q + 1]));
       }
     }
     const float y[8] = {acc[0].x, acc[0].y, acc[1].x, acc[1].y, acc[2].x, acc[2].y, acc[3].x, acc[3].y};
@@ -117,7 +125,7 @@ __global__ void __launch_bounds__(kCbThreads, 3) combine_kernel(const CbParams p
     } else {
 #pragma unroll
       for (int q = 0; q < 8; ++q)
-        if (q < here) o[q] = mx_from_float<O>(y[q]);
+        if (q < here) o[32 * q] = mx_from_float<O>(y[q]);
     }
   }
 }

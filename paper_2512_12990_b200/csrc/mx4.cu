@@ -33,7 +33,6 @@ template <>
 struct MxRaw<float> {
   float4 a, b;
   __device__ __forceinline__ void load(const float* p) { a = __ldcg(reinterpret_cast<const float4*>(p)), b = __ldcg(reinterpret_cast<const float4*>(p) + 1); }
-  __device__ __forceinline__ void one_by_one(const float* p) { a = make_float4(__ldcg(p), __ldcg(p + 1), __ldcg(p + 2), __ldcg(p + 3)), b = make_float4(__ldcg(p + 4), __ldcg(p + 5), __ldcg(p + 6), __ldcg(p + 7)); }
   __device__ __forceinline__ void values(float (&v)[8]) const { v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w; }
   __device__ __forceinline__ uint32_t largest() const {
     float v[8];
@@ -48,12 +47,6 @@ template <class T>
 struct MxRaw {  // 16 bits: two to a word
   uint4 a;
   __device__ __forceinline__ void load(const T* p) { a = __ldcg(reinterpret_cast<const uint4*>(p)); }
-  __device__ __forceinline__ void one_by_one(const T* p) {
-    uint32_t h[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) h[j] = __ldcg(reinterpret_cast<const unsigned short*>(p) + j);
-    a = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
-  }
   __device__ __forceinline__ void values(float (&v)[8]) const {
     const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
@@ -73,6 +66,34 @@ struct MxRaw {  // 16 bits: two to a word
   }
 };
 
+// A run whose row does not begin on 16 bytes: the warp loads it 32 neighbouring values at a time and swaps them about in shared memory.
+template <class T>
+struct MxScattered {
+  T v[8];
+  __device__ __forceinline__ void load(const T* run, int lane, int n) {  // n: values of the run that there are
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      if (32 * q + lane >= n) continue;
+      if constexpr (sizeof(T) == 4) {
+        v[q] = __ldcg(run + 32 * q + lane);
+      } else {
+        const unsigned short h = __ldcg(reinterpret_cast<const unsigned short*>(run) + 32 * q + lane);
+        memcpy(&v[q], &h, 2);
+      }
+    }
+  }
+  __device__ __forceinline__ MxRaw<T> gather(T* room, int lane, int n) const {
+    MxRaw<T> raw;
+    __syncwarp();
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      if (32 * q + lane < n) room[32 * q + lane] = v[q];
+    __syncwarp();
+    memcpy(&raw, __builtin_assume_aligned(room + 8 * lane, 16), sizeof(raw));
+    return raw;
+  }
+};
+
 // Four lanes hold a block of 32 values, eight each: the largest magnitude by two exchanges, then each lane writes the four bytes
 // of its eight codes (a warp's stores are 128 consecutive bytes) and the first the scale.  LINEAR: the rows are one behind the other
 // and whole runs, so that a place is a shift of a counter.  Bound: the values read.
@@ -88,15 +109,27 @@ __global__ void __launch_bounds__(kMxThreads) mx_quantize_kernel(const T* __rest
     if constexpr (!LINEAR) mx_runs(first, rows, per_row, K, lane, run);
     const int64_t at = first * 256 + lane * 8;
     MxRaw<T> raw[kMxAhead];
+    if constexpr (WIDE) {
 #pragma unroll
-    for (int i = 0; i < kMxAhead; ++i) {
-      if constexpr (LINEAR) {
-        if (first + i < runs) raw[i].load(x + at + 256 * i);
-      } else if (run[i].live) {
-        const T* src = x + run[i].row * ld + run[i].c;
-        if constexpr (WIDE) raw[i].load(src);
-        else raw[i].one_by_one(src);
+      for (int i = 0; i < kMxAhead; ++i) {
+        if constexpr (LINEAR) {
+          if (first + i < runs) raw[i].load(x + at + 256 * i);
+        } else if (run[i].live) {
+          raw[i].load(x + run[i].row * ld + run[i].c);
+        }
       }
+    } else {
+      __shared__ __align__(16) T room[kMxThreads / 32][256];
+      MxScattered<T> loose[kMxAhead];
+      int n[kMxAhead];
+#pragma unroll
+      for (int i = 0; i < kMxAhead; ++i) {  // the same row and run in all lanes
+        const int c0 = run[i].c - lane * 8;
+        n[i] = run[i].row < rows ? min(256, K - c0) : 0;
+        loose[i].load(x + (n[i] > 0 ? run[i].row * ld + c0 : 0), lane, n[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < kMxAhead; ++i) raw[i] = loose[i].gather(room[threadIdx.x >> 5], lane, n[i]);
     }
 #pragma unroll
     for (int i = 0; i < kMxAhead; ++i) {
