@@ -141,28 +141,59 @@ struct MpPlaceParams {
   int *first, *list;    // first: [3][E + 1], rows, tiles and tiles' rows before an expert
   uint8_t *t_codes, *t_scale;
   int pairs, E, blocks, chunk, tile, k, x_per_pair, K;
+  MpHeader* head;
 };
 // Each pair's row to its place in its tile; scales as those of packed weights.  A block takes `chunk` pairs of one block of ranks: where they
-// go is worked out by a thread each, then a warp moves four rows at a time.  A row is read in runs of 512 bytes and written in runs of
+// go is worked out by a thread each, then a warp moves two or four rows at a time.  A row is read in runs of 512 bytes and written in runs of
 // 128, which is what the swizzled operand layout keeps together.  (Without the swizzle a row's pieces of 16 bytes lie apart: 9 us
 // for 8,192 rows of 2,048 values and 28 for 49,152 of 1,408, in whichever order the rows are taken.)
-constexpr int kMpPlaceRows = 4, kMpPlaceChunk = 128;
+constexpr int kMpPlaceChunk = 128;
 struct MpPlace {
   uint32_t x, code, scale, row;  // row of x (all ones: none); rows, and blocks of scales, before the tile; rows of the tile << 16 | row in it
 };
-__global__ void __launch_bounds__(kMpPlaceThreads, 4) mp_place_kernel(const MpPlaceParams p) {
+// FEW: no kernel has ranked the pairs; every block looks at all of them, which takes less than a launch up to kMpSortPairs, and takes 32
+// of them itself.  (300 tokens x 6: 5.8 us for two launches, and 2 to 3 of the 10 to 13 us of small calls.)
+template <bool FEW>
+__global__ void __launch_bounds__(FEW ? 2 * kMpPlaceThreads : kMpPlaceThreads, FEW ? 2 : 4) mp_place_kernel(const MpPlaceParams p) {
+  constexpr int kThreads = FEW ? 2 * kMpPlaceThreads : kMpPlaceThreads, kRows = FEW ? 2 : 4;
   __shared__ int s_first[kMpMaxExperts], s_before[kMpMaxExperts], s_count[kMpMaxExperts], s_tile[kMpMaxExperts], s_row[kMpMaxExperts], s_sums[32][3];
   __shared__ MpPlace s_place[kMpPlaceChunk];
   mx_dep_launch();
+  if constexpr (FEW)
+    for (int e = threadIdx.x; e < p.E; e += kThreads) s_count[e] = s_before[e] = 0;
   mx_dep_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int base = blockIdx.x * p.chunk, me = base / kMpSortPairs;
+  int own = -1, own_rank = 0;
+  if constexpr (FEW) {
+    __syncthreads();
+    if (tid < 32 && base + tid < p.pairs) own = __ldcg(p.ids + base + tid);
+    constexpr int kAhead = kMpSortPairs / kThreads;
+    int id[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) id[i] = i * kThreads + tid < p.pairs ? __ldcg(p.ids + i * kThreads + tid) : -1;
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int at = i * kThreads + tid;
+      if ((unsigned)id[i] < (unsigned)p.E) {
+        atomicAdd(&s_count[id[i]], 1);
+        if (at < base) atomicAdd(&s_before[id[i]], 1);
+      } else {
+        bad |= at < p.pairs;
+      }
+    }
+    if (bad && blockIdx.x == 0) atomicOr(&p.head->status, (unsigned)SLICEMOE_STATUS_BAD_EXPERT_ID);
+    __syncthreads();
+  }
   int sum[3] = {};
-  for (int e0 = 0; e0 < p.E; e0 += kMpPlaceThreads) {
+  for (int e0 = 0; e0 < p.E; e0 += kThreads) {
     const int e = e0 + tid;
     int count = 0, before = 0;
     if (e < p.E) {
-      if (p.ids) {
+      if constexpr (FEW) {
+        count = s_count[e], before = s_before[e];
+      } else if (p.ids) {
 #pragma unroll 8
         for (int b = 0; b < p.blocks; ++b) {
           const int n = __ldcg(p.hist + (size_t)b * p.E + e);
@@ -175,7 +206,7 @@ __global__ void __launch_bounds__(kMpPlaceThreads, 4) mp_place_kernel(const MpPl
     }
     const MpTiles t = mp_tiles(count, p.tile);
     int v[3] = {count, t.n, t.n * t.each}, total[3];
-    mp_scan3<kMpPlaceThreads>(v, s_sums, total);
+    mp_scan3<kThreads>(v, s_sums, total);
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
       v[i] += sum[i];
@@ -190,12 +221,16 @@ __global__ void __launch_bounds__(kMpPlaceThreads, 4) mp_place_kernel(const MpPl
   const int atoms = mx_atoms(p.K), pieces = 2 * mx_chunks(p.K), kbytes = p.K >> 1, halves = (p.tile + 127) >> 7, steps = mp_steps(p.K);
   for (int c0 = 0; c0 < p.chunk; c0 += kMpPlaceChunk) {
     const int here = min(kMpPlaceChunk, p.chunk - c0);
+    if constexpr (FEW) {
+      if (warp == 0) own_rank = __popc(__match_any_sync(0xffffffffu, own) & ((1u << lane) - 1u));  // in their order
+    }
     __syncthreads();
     if (tid < here) {
       const int pair = base + c0 + tid;
       MpPlace at = {0xffffffffu, 0, 0, 0};
       if (pair < p.pairs) {
-        const int e = p.ids ? __ldcg(p.ids + pair) : 0, rank = p.ids ? __ldcg(p.rank + pair) : pair;
+        int e = own, rank = own_rank;
+        if constexpr (!FEW) e = p.ids ? __ldcg(p.ids + pair) : 0, rank = p.ids ? __ldcg(p.rank + pair) : pair;
         if ((unsigned)e < (unsigned)p.E) {
           const int pos = p.ids ? s_before[e] + rank : pair, count = s_count[e];
           const MpTiles t = count <= p.tile ? MpTiles{1, (count + 15) & ~15} : mp_tiles(count, p.tile);
@@ -210,31 +245,31 @@ __global__ void __launch_bounds__(kMpPlaceThreads, 4) mp_place_kernel(const MpPl
       s_place[tid] = at;
     }
     __syncthreads();
-    for (int i = warp * kMpPlaceRows; i < here; i += kMpPlaceThreads / 32 * kMpPlaceRows) {
+    for (int i = warp * kRows; i < here; i += kThreads / 32 * kRows) {
       // loads first, then stores: left to itself the compiler cannot know that they do not overlap, and waits for each
       for (int q = lane; q < pieces; q += 32) {
-        uint4 v[kMpPlaceRows];
+        uint4 v[kRows];
 #pragma unroll
-        for (int l = 0; l < kMpPlaceRows; ++l) {
+        for (int l = 0; l < kRows; ++l) {
           const uint32_t x = s_place[i + l].x;
           v[l] = ~x && q * 16 < kbytes ? __ldcg(reinterpret_cast<const uint4*>(p.codes + (size_t)x * kbytes) + q) : make_uint4(0, 0, 0, 0);
         }
 #pragma unroll
-        for (int l = 0; l < kMpPlaceRows; ++l) {
+        for (int l = 0; l < kRows; ++l) {
           const MpPlace at = s_place[i + l];
           if (~at.x) *reinterpret_cast<uint4*>(p.t_codes + (size_t)at.code * steps * kMpRowBytes + mp_piece(at.row >> 16, at.row & 0xffffu, q)) = v[l];
         }
       }
       for (int j = lane; j < atoms; j += 32) {
         const int left = (p.K >> 5) - 4 * j;
-        uint32_t w[kMpPlaceRows];
+        uint32_t w[kRows];
 #pragma unroll
-        for (int l = 0; l < kMpPlaceRows; ++l) {
+        for (int l = 0; l < kRows; ++l) {
           const uint32_t x = s_place[i + l].x;
           w[l] = ~x ? __ldcg(reinterpret_cast<const uint32_t*>(p.scale + (size_t)x * (4 * atoms)) + j) : 0u;
         }
 #pragma unroll
-        for (int l = 0; l < kMpPlaceRows; ++l) {
+        for (int l = 0; l < kRows; ++l) {
           const MpPlace at = s_place[i + l];
           const uint32_t r = at.row & 0xffffu;
           if (left < 4) w[l] &= (1u << (8 * left)) - 1u;  // bytes beyond the row's end
@@ -908,14 +943,16 @@ extern "C" int slicemoe_mx4_product(const slicemoe_mx4_mat* mats, int n_experts,
   if (placed) {
     int *rank = reinterpret_cast<int*>(ws + l.rank), *hist = reinterpret_cast<int*>(ws + l.hist), *first = reinterpret_cast<int*>(ws + l.first),
         *list = reinterpret_cast<int*>(ws + l.list);
-    if (ids) {
+    const bool few = ids && pairs <= kMpSortPairs;
+    if (ids && !few) {
       const int rc = mx_launch(mp_sort_kernel, dim3(l.blocks), kMpSortThreads, 0, st, MpSortParams{ids, pairs, E, rank, hist, p.head});
       if (rc != SLICEMOE_OK) return rc;
     }
-    int chunk = kMpPlaceThreads / 32 * kMpPlaceRows;  // pairs of a block: more where there are blocks enough to fill the device
-    while (chunk < kMpSortPairs && pairs / chunk > 148 * 6) chunk *= 2;
-    const MpPlaceParams pp = {ids, rank, hist, codes, scale, first, list, ws + l.codes, ws + l.scale, pairs, E, l.blocks, chunk, p.tile, k, p.x_per_pair, K};
-    const int rc = mx_launch(mp_place_kernel, dim3((pairs + chunk - 1) / chunk), kMpPlaceThreads, 0, st, MpPlaceParams(pp));
+    int chunk = 32;  // pairs of a block: more where there are blocks enough to fill the device
+    while (!few && chunk < kMpSortPairs && pairs / chunk > 148 * 6) chunk *= 2;
+    const MpPlaceParams pp = {ids, rank, hist, codes, scale, first, list, ws + l.codes, ws + l.scale, pairs, E, l.blocks, chunk, p.tile, k, p.x_per_pair, K, p.head};
+    const int rc = mx_launch(few ? mp_place_kernel<true> : mp_place_kernel<false>, dim3((pairs + chunk - 1) / chunk),
+                             (unsigned)(few ? 2 * kMpPlaceThreads : kMpPlaceThreads), 0, st, MpPlaceParams(pp));
     if (rc != SLICEMOE_OK) return rc;
     p.first = first;
     p.list = list;
