@@ -16,10 +16,10 @@
  *     One kind of work is excepted.  A layer call of up to three tokens (slicemoe_decode_step_host's too) reads the shared
  *     experts' table and slices - with SLICEMOE_LISTS_RESIDENT all experts' - without waiting for a kernel that lets its
  *     dependents start early (programmatic dependent launch: griddepcontrol.launch_dependents,
- *     cudaTriggerProgrammaticLaunchCompletion).  A kernel of the caller's that does so must not write expert tables or
- *     weights, unless other work is enqueued between it and the call: a kernel that does not, a copy, or slicemoe_pack
- *     (not slicemoe_route_topk, another layer call, or one of the calls for microscaled experts but slicemoe_mx4_pack).  Ordinary kernels, copies and slicemoe_pack may write them
- *     directly ahead of the call.
+ *     cudaTriggerProgrammaticLaunchCompletion), and slicemoe_mx4_product its table of matrices (not the matrices).  A kernel of
+ *     the caller's that does so must not write expert tables or weights, unless other work is enqueued between it and the call:
+ *     a kernel that does not, a copy, slicemoe_pack or slicemoe_mx4_pack (not slicemoe_route_topk, another layer call, or another
+ *     of the calls for microscaled experts).  Ordinary kernels, copies and the two packs may write them directly ahead of the call.
  *   - Weight matrices are row-major [N, K] (N outputs, K inputs = contraction axis); quantisation
  *     groups run along K.
  *
@@ -452,7 +452,7 @@ int slicemoe_mx4_dequantize(const uint8_t *codes, const uint8_t *scale, int rows
  * quantised as by slicemoe_mx4_quantize into buffers of slicemoe_mx4_codes_bytes / slicemoe_mx4_scale_bytes bytes.
  * slicemoe_mx4_unpack - test hook and dump helper: the codes and scales of gate (part 0; a plain matrix) or up (part 1) as
  * slicemoe_mx4_quantize writes them.
- * Errors: INVALID_ARG (null, N <= 0, K <= 0, K % 32, ld < K, alignment), UNSUPPORTED (dtype; N > 2^24 or K > 2^20), CUDA.
+ * Errors: INVALID_ARG (null, N <= 0, K <= 0, K % 32, ld < K, alignment), UNSUPPORTED (dtype; N > 2^21 or K > 2^20), CUDA.
  */
 typedef struct slicemoe_mx4_mat {
   const uint8_t *codes, *scale;
@@ -486,7 +486,7 @@ int slicemoe_mx4_unpack(const uint8_t *codes, const uint8_t *scale, int N, int K
  *              time; two calls that may overlap, or two graphs that may run at once, need one each.  One for larger T, k, n_experts or
  *              K serves smaller calls too.  It holds the token rows in the order of the experts: about T k K / 2 bytes
  * A row's result does not depend on the other rows of the call, bit for bit, and is reproducible.
- * Errors: INVALID_ARG (null, sizes, alignment, workspace too small), UNSUPPORTED (n_experts > 1024, T k > 2^24, N > 2^24,
+ * Errors: INVALID_ARG (null, sizes, alignment, workspace too small), UNSUPPORTED (n_experts > 1024, T k > 2^24, N > 2^21,
  * K > 2^20, k > SLICEMOE_MAX_TOP_K, dtype), CUDA.
  */
 size_t slicemoe_mx4_workspace_bytes(int T, int k, int n_experts, int K);

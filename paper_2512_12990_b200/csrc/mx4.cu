@@ -325,7 +325,7 @@ extern "C" int slicemoe_mx4_pack(const void* W, const void* up, int dtype, int N
   if (!mx_aligned(scale, 16)) return SLICEMOE_E_INVALID_ARG;
   if (!mx_sizes(N, K)) return SLICEMOE_E_UNSUPPORTED;
   const dim3 grid(mx_atoms(K), mx_row_blocks(N, up != nullptr));
-  if (grid.y > 65535u) return SLICEMOE_E_UNSUPPORTED;
+  static_assert(2ll * kMxMaxN / kMxRows + 1 <= 65535, "row blocks in a grid's second dimension");
   cudaStream_t st = (cudaStream_t)stream;
   if (dtype == SLICEMOE_F32)
     mx_pack_kernel<float><<<grid, kMxThreads, 0, st>>>(static_cast<const float*>(W), static_cast<const float*>(up), N, K, ld, codes, scale);

@@ -16,7 +16,7 @@ constexpr int kMxChunk = 64;    // values of a chunk: what one tensor instructio
 constexpr int kMxChunkBytes = kMxRows * kMxChunk / 2;
 constexpr int kMxAtomK = 128;   // values whose scales lie together
 constexpr int kMxAtomBytes = kMxRows * kMxAtomK / kMxBlock;
-constexpr int kMxMaxN = 1 << 24, kMxMaxK = 1 << 20;
+constexpr int kMxMaxN = 1 << 21, kMxMaxK = 1 << 20;
 
 __host__ __device__ inline int mx_chunks(int K) { return (K + kMxChunk - 1) / kMxChunk; }
 __host__ __device__ inline int mx_atoms(int K) { return (K + kMxAtomK - 1) / kMxAtomK; }

@@ -144,7 +144,8 @@ class Case:
 
 @pytest.mark.parametrize("T,k,E,N,K", [
     (1, 1, 1, 1, 32), (1, 1, 1, 128, 64), (1, 6, 8, 100, 96), (1, 2, 4, 256, 2048), (3, 2, 5, 129, 160), (16, 4, 9, 64, 256), (17, 1, 1, 130, 416),
-    (40, 3, 2, 200, 128), (224, 1, 1, 128, 128), (225, 1, 1, 128, 192), (300, 2, 3, 257, 288), (500, 2, 70, 48, 320), (2100, 4, 6, 32, 64), (5, 16, 40, 272, 1408)])
+    (40, 3, 2, 200, 128), (224, 1, 1, 128, 128), (225, 1, 1, 128, 192), (300, 2, 3, 257, 288), (500, 2, 70, 48, 320), (2100, 4, 6, 32, 64), (5, 16, 40, 272, 1408),
+    (20, 3, 200, 32, 96), (400, 2, 1024, 16, 64), (4, 2, 1000, 48, 64)])
 @pytest.mark.parametrize("gated", [False, True])
 def test_product_matches_the_oracle(T, k, E, N, K, gated):
     c = Case(T, k, E, N, K, gated)
@@ -286,6 +287,37 @@ def test_product_in_a_graph_on_another_stream(T):
         out.zero_()
         g.replay()
     c.check(out, ids=((c.ids + 1) % 8).astype(np.int32))
+
+
+def test_calls_on_two_streams_with_a_workspace_each():
+    import torch
+    from paper_2512_12990_b200 import binding as B
+    c = Case(900, 3, 8, 160, 192, gated=True)
+    (codes, scale), ids, ref = c.dev(), _t(c.ids), c.run()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    spaces = [B.new_mx4_workspace(900, 3, 8) for _ in range(2)]
+    outs = [torch.empty_like(ref) for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for st, ws, out in zip(streams, spaces, outs):
+            B.slicemoe_mx4_product(c.table, codes, scale, ids, ws, out=out, stream=st)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, ref) for o in outs) and all(B.slicemoe_get_status(ws) == 0 for ws in spaces)
+
+
+def test_a_call_right_behind_the_one_that_makes_its_input():
+    """Kernels overlap; what one writes the next must see: quantise into the same buffers and multiply, over and over."""
+    import torch
+    from paper_2512_12990_b200 import binding as B
+    for T in (1, 60, 700):
+        c = Case(T, 2, 4, 96, 256)
+        ids = _t(c.ids)
+        xs = [torch.randn(T, 256, device="cuda") for _ in range(6)]
+        refs = [B.slicemoe_mx4_product(c.table, *B.slicemoe_mx4_quantize(x), ids, c.ws, dtype=torch.float32) for x in xs]
+        torch.cuda.synchronize()
+        for _ in range(10):
+            got = [B.slicemoe_mx4_product(c.table, *B.slicemoe_mx4_quantize(x), ids, c.ws, dtype=torch.float32) for x in xs]
+            assert all(torch.equal(a, b) for a, b in zip(got, refs))
 
 
 def test_workspace_of_a_larger_call_serves_smaller_ones():

@@ -106,7 +106,7 @@ def test_a_short_limit_is_not_spent_on_the_launch_before():
     assert B.slicemoe_get_status(ws) == 0
 
 
-@pytest.mark.parametrize("T", [2, 300])
+@pytest.mark.parametrize("T", [2, 300, 3000])
 def test_the_product_of_microscaled_experts_gives_up_by_itself(T):
     """The waits for weights that are never brought run out: the call returns, the status says so, and the workspace serves on once
     the switch is off again."""
