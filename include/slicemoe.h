@@ -499,7 +499,7 @@ int slicemoe_mx4_product(const slicemoe_mx4_mat *mats, int n_experts, int N, int
  * slicemoe_combine - the end of a layer: out[t] = base[t] + sum_j weights[t, j] rows[t, j], added up in fp32 in list order, rounded
  * once.
  *   rows       device [T, k, N] of rows_dtype; weights device float32 [T, k]
- *   ids        device int32 [T, k] or NULL: pairs whose id is outside [0, n_experts) are left out (their rows are not read)
+ *   ids        device int32 [T, k] or NULL: pairs whose id is outside [0, n_experts) are left out, whatever their rows hold
  *   base       device [T, N] of out_dtype or NULL (a residual, or the shared experts' part); may be out itself
  *   out        device [T, N] of out_dtype
  * Arrays are aligned to their element type.  Errors: INVALID_ARG (null, T <= 0, N <= 0, k < 1, n_experts <= 0 with ids,

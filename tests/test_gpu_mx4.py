@@ -362,14 +362,43 @@ def test_combine_matches_the_oracle(T, k, N, rd, od, base, listed):
     if listed:
         rows[_t((ids < 0) | (ids >= 4))] = float("nan")        # not to be read
     out = B.slicemoe_combine(rows, _t(w), None if ids is None else _t(ids), 4, b, _dt(od))
-    y = mx4.combine(_f64(rows), w, ids, 4, None if b is None else _f64(b))
-    mag = mx4.combine(np.abs(np.nan_to_num(_f64(rows))), np.abs(w), ids, 4, None if b is None else np.abs(_f64(b)))
+    r, keep = np.nan_to_num(_f64(rows)), w.astype(np.float64) * (1 if ids is None else (ids >= 0) & (ids < 4))
+    y, mag = np.einsum("tkn,tk->tn", r, keep), np.einsum("tkn,tk->tn", np.abs(r), np.abs(keep))
+    if base:
+        y, mag = y + _f64(b), mag + np.abs(_f64(b))
+    assert T > 100 or np.allclose(y, mx4.combine(_f64(rows), w, ids, 4, None if b is None else _f64(b)), rtol=1e-12, atol=1e-12)
     tol = (k + 1) * 2.0 ** -24 * mag
     tol = tol + _half_step(np.abs(y) + tol, od) + 2.0 ** -126
     assert (np.abs(_f64(out) - y) <= tol).all()
     if base:                                                    # in place
         same = B.slicemoe_combine(rows, _t(w), None if ids is None else _t(ids), 4, b, out=b)
         assert same is b and torch.equal(b, out)
+
+
+@pytest.mark.parametrize("T,k,N,rd,od,listed", [(4100, 7, 2056, "bf16", "bf16", True), (12000, 3, 1672, "f16", "f32", False), (30001, 8, 264, "bf16", "f16", True)])
+def test_combine_of_more_rows_than_l2_holds(T, k, N, rd, od, listed):
+    """The same bound, in fp64 on the device; and in place."""
+    import torch
+    from paper_2512_12990_b200 import binding as B
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(T)
+    rows = torch.randn(T, k, N, device="cuda", generator=gen).to(_dt(rd))
+    w, base = torch.randn(T, k, device="cuda", generator=gen), torch.randn(T, N, device="cuda", generator=gen).to(_dt(od))
+    ids = torch.randint(-1, 6, (T, k), device="cuda", generator=gen, dtype=torch.int32) if listed else None
+    keep = w.double() if ids is None else w.double() * ((ids >= 0) & (ids < 5))
+    y = torch.einsum("tkn,tk->tn", rows.double(), keep) + base.double()
+    mag = torch.einsum("tkn,tk->tn", rows.double().abs(), keep.abs()) + base.double().abs()
+    tol = (k + 1) * 2.0 ** -24 * mag + 2.0 ** -126
+    if od != "f32":
+        tol = tol + (y.abs() + tol) * torch.finfo(_dt(od)).eps / 2 + 2.0 ** -25
+    if ids is not None:
+        rows[(ids < 0) | (ids >= 5)] = float("nan")
+    out = B.slicemoe_combine(rows, w, ids, 5, base, _dt(od))
+    assert ((out.double() - y).abs() <= tol).all()
+    none = B.slicemoe_combine(rows, w, ids, 5, None, _dt(od))
+    assert ((none.double() - (y - base.double())).abs() <= tol + mag * 2.0 ** -8).all()
+    B.slicemoe_combine(rows, w, ids, 5, base, out=base)
+    assert torch.equal(base, out)
 
 
 # ---- a layer of them ------------------------------------------------------------------------------------------------
