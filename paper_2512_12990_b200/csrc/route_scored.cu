@@ -172,10 +172,10 @@ __device__ __forceinline__ double rs_total(const RsParams& p, const float* logit
 
 // The order of the first `n` candidates (lane j holds one, id) by their keys in 64 bits; lane j gets the j-th of them.
 template <bool SIGMOID>
-__device__ __noinline__ int rs_reorder(const RsParams& p, const float* logits, float vmax, int id, int n, int lane) {
+__device__ __noinline__ int rs_reorder(const RsParams& p, const float* logits, const float* bias, float vmax, int id, int n, int lane) {
   const double total = rs_total<SIGMOID>(p, logits, vmax, lane);
   double key = -CUDART_INF;
-  if (lane < n) key = rs_score<SIGMOID>(logits[id], vmax, total) + (double)__ldcg(p.bias + id);
+  if (lane < n) key = rs_score<SIGMOID>(logits[id], vmax, total) + (double)bias[id];
   if (isnan(key)) key = -CUDART_INF;
   int rank = 0;
 #pragma unroll 1
@@ -193,24 +193,36 @@ __device__ __noinline__ int rs_reorder(const RsParams& p, const float* logits, f
   return mine;
 }
 
-// The whole choice with keys in 64 bits: k rounds of the largest key, the lowest index that has it.  Lane j < k gets selection j.
+// A token's keys in 64 bits, and which groups are kept by them, as a bit mask.
 template <bool SIGMOID>
-__device__ __noinline__ int rs_exact(const RsParams& p, const float* logits, double* keys, float vmax, int lane) {
+__device__ __noinline__ uint32_t rs_exact_keys(const RsParams& p, const float* logits, const float* bias, double* keys, float vmax, int lane) {
   const double total = rs_total<SIGMOID>(p, logits, vmax, lane);
-#pragma unroll 1
-  for (int e = lane; e < p.E; e += 32) {
-    double key = rs_score<SIGMOID>(logits[e], vmax, total);
-    if (p.bias) key += (double)__ldcg(p.bias + e);
-    keys[e] = isnan(key) ? -CUDART_INF : key;
+  // four at a time: an exponential and a quotient in fp64 are a thousand clocks one after the other
+  for (int e0 = lane; e0 < p.E; e0 += 128) {
+    double key[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) key[i] = rs_score<SIGMOID>(logits[min(e0 + 32 * i, p.E - 1)], vmax, total);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int e = e0 + 32 * i;
+      if (e >= p.E) break;
+      if (p.bias) key[i] += (double)bias[e];
+      keys[e] = isnan(key[i]) ? -CUDART_INF : key[i];
+    }
   }
   __syncwarp();
-  uint32_t kept = 0xffffffffu;
-  if (p.n_group > 1) kept = rs_groups(p, (const double*)keys, lane, 0.0f, nullptr);
+  const uint32_t kept = p.n_group > 1 ? rs_groups(p, (const double*)keys, lane, 0.0f, nullptr) : 0xffffffffu;
   __syncwarp();
+  return kept;
+}
+
+// The choice with keys in 64 bits where more than 32 of them are near one another: k rounds of the largest key, the lowest index that has
+// it.  Lane j < k gets selection j.
+__device__ __noinline__ int rs_exact_choice(const RsParams& p, double* keys, uint32_t kept, int lane) {
+  if (p.n_group > 1) {
 #pragma unroll 1
-  for (int e = lane; e < p.E; e += 32) {
-    if (!p.bias) keys[e] = (double)logits[e];  // within the groups the logits' order is exact, and finer than that of their scores
-    if (p.n_group > 1 && !rs_kept(p, kept, e)) keys[e] = CUDART_NAN;  // out of the choice
+    for (int e = lane; e < p.E; e += 32)
+      if (!rs_kept(p, kept, e)) keys[e] = CUDART_NAN;  // out of the choice
   }
   int id = 0;
 #pragma unroll 1
@@ -251,13 +263,15 @@ __device__ __forceinline__ void rs_sort(uint32_t (&a)[N]) {
 
 template <int VPT, bool SIGMOID>
 __global__ void __launch_bounds__(32 * kRsWarps, VPT <= 8 ? 8 : 4) route_scored_kernel(const RsParams p) {
-  __shared__ __align__(16) double s_keys[kRsWarps][32 * VPT];  // a token's keys in 32 bits, or in 64
+  __shared__ __align__(16) uint32_t s_keys[kRsWarps][32 * VPT];
+  __shared__ double s_exact[kRsWarps][32 * VPT];
   __shared__ __align__(16) float s_logits[kRsWarps][32 * VPT];
+  __shared__ float s_bias[32 * VPT];
   mx_dep_launch();
   mx_dep_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   constexpr float near = SIGMOID ? kNearSigmoid : kNearSoftmax;
-  uint32_t* keys = reinterpret_cast<uint32_t*>(s_keys[warp]);
+  uint32_t* keys = s_keys[warp];
   float* logits = s_logits[warp];
   const int stride = gridDim.x * kRsWarps;
   int t = blockIdx.x * kRsWarps + warp;
@@ -266,12 +280,10 @@ __global__ void __launch_bounds__(32 * kRsWarps, VPT <= 8 ? 8 : 4) route_scored_
   if (p.bias) {
     // read once a block, in whole lines: the same kilobyte read by every warp for itself, eight values apart, kept a few L2 slices busy
     // for 19 of 28 us (8,192 tokens of 256 experts)
-    float* all = s_logits[0];
-    for (int e = threadIdx.x; e < 32 * VPT; e += 32 * kRsWarps) all[e] = e < p.E ? __ldcg(p.bias + e) : 0.0f;
+    for (int e = threadIdx.x; e < 32 * VPT; e += 32 * kRsWarps) s_bias[e] = e < p.E ? __ldcg(p.bias + e) : 0.0f;
     __syncthreads();
 #pragma unroll
-    for (int v = 0; v < VPT; ++v) bias[v] = all[lane * VPT + v];
-    __syncthreads();
+    for (int v = 0; v < VPT; ++v) bias[v] = s_bias[lane * VPT + v];
   }
   if (t >= p.T) return;
   for (; t < p.T; t += stride) {
@@ -323,13 +335,16 @@ __global__ void __launch_bounds__(32 * kRsWarps, VPT <= 8 ? 8 : 4) route_scored_
       for (int v = 0; v < VPT; ++v)
         logits[lane * VPT + v] = p.bias ? rs_value(key[v]) : (sums ? score(val[v]) : val[v]);
       __syncwarp();
-      const uint32_t kept = rs_groups(p, (const float*)logits, lane, near, sums ? &unsure : nullptr);
+      uint32_t kept = rs_groups(p, (const float*)logits, lane, near, sums ? &unsure : nullptr);
       __syncwarp();
 #pragma unroll
-      for (int v = 0; v < VPT; ++v) {
-        logits[lane * VPT + v] = val[v];
+      for (int v = 0; v < VPT; ++v) logits[lane * VPT + v] = val[v];
+      __syncwarp();
+      if (unsure) kept = rs_exact_keys<SIGMOID>(p, logits, s_bias, s_exact[warp], vmax, lane);
+      unsure = false;
+#pragma unroll
+      for (int v = 0; v < VPT; ++v)
         if (lane * VPT + v < p.E && !rs_kept(p, kept, lane * VPT + v)) a[v] = keys[lane * VPT + v] = 0u;
-      }
     }
     rs_sort<VPT>(a);
     if (p.n_group > 1 && p.lanes > 0) {
@@ -355,10 +370,13 @@ __global__ void __launch_bounds__(32 * kRsWarps, VPT <= 8 ? 8 : 4) route_scored_
         const uint32_t v = __shfl_sync(0xffffffffu, order, o * size);
         rank += v > order || (v == order && o < me);
       }
-      const bool kept = real && rank < p.topk_group;
+      bool kept = real && rank < p.topk_group;
       if (sums && p.topk_group < groups) {
         const uint32_t low = __reduce_min_sync(0xffffffffu, kept ? order : 0xffffffffu), high = __reduce_max_sync(0xffffffffu, kept ? 0u : order);
-        unsure = rs_near(rs_value(low), rs_value(high), 2.0f * near);
+        if (rs_near(rs_value(low), rs_value(high), 2.0f * near)) {  // the same in all lanes
+          __syncwarp();
+          kept = real && ((rs_exact_keys<SIGMOID>(p, logits, s_bias, s_exact[warp], vmax, lane) >> me) & 1u);
+        }
       }
       if (!kept) {
 #pragma unroll
@@ -381,8 +399,8 @@ __global__ void __launch_bounds__(32 * kRsWarps, VPT <= 8 ? 8 : 4) route_scored_
     int chosen = p.k + (p.bias != nullptr);
     for (int j = 0; j < chosen; ++j) choose(j);
     uint32_t next = __shfl_down_sync(0xffffffffu, my_top, 1);
-    bool close = false, all = unsure;  // whether selections have to be put in order, or the whole choice made again, in 64 bits
-    if (p.bias && !all) {
+    bool close = false, all = false;  // whether selections have to be put in order, or the whole choice made again, in 64 bits
+    if (p.bias) {
       close = __any_sync(0xffffffffu, lane < p.k && next != 0u && rs_near(rs_value(my_top), rs_value(next), near));
       if (close) {  // more candidates, until the last is clearly behind the k-th
         const float kth = rs_value(__shfl_sync(0xffffffffu, my_top, p.k - 1));
@@ -401,7 +419,8 @@ __global__ void __launch_bounds__(32 * kRsWarps, VPT <= 8 ? 8 : 4) route_scored_
     int id;
     if (all) {  // the same in all lanes
       __syncwarp();
-      id = rs_exact<SIGMOID>(p, logits, s_keys[warp], vmax, lane);
+      const uint32_t kept = rs_exact_keys<SIGMOID>(p, logits, s_bias, s_exact[warp], vmax, lane);
+      id = rs_exact_choice(p, s_exact[warp], kept, lane);
     } else {
       const bool tied = __any_sync(0xffffffffu, lane + 1 < chosen && next == my_top);
       int skip = 0;  // of equal keys in one lane, which one
@@ -420,7 +439,7 @@ __global__ void __launch_bounds__(32 * kRsWarps, VPT <= 8 ? 8 : 4) route_scored_
       }
       if (close) {
         const int n = __popc(__ballot_sync(0xffffffffu, lane < chosen && my_top != 0u));
-        id = rs_reorder<SIGMOID>(p, logits, vmax, id, n, lane);
+        id = rs_reorder<SIGMOID>(p, logits, s_bias, vmax, id, n, lane);
       }
     }
     __syncwarp();
@@ -460,7 +479,8 @@ static int rs_launch(RsParams p, cudaStream_t st) {
   p.lanes = 0;
   if (size % vpt == 0 && ((size / vpt) & (size / vpt - 1)) == 0) p.lanes = size / vpt;
   const int blocks = (p.T + kRsWarps - 1) / kRsWarps, most = 148 * (vpt <= 8 ? 8 : 4);  // as many as are resident together
-  return mx_launch(kernel, dim3(blocks < most ? blocks : most), 32 * kRsWarps, 0, st, RsParams(p));
+  const int rounds = (blocks + most - 1) / most;  // of tokens to a warp: the same for all
+  return mx_launch(kernel, dim3((blocks + rounds - 1) / rounds), 32 * kRsWarps, 0, st, RsParams(p));
 }
 
 }  // namespace slicemoe
