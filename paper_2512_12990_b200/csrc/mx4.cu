@@ -159,36 +159,46 @@ __global__ void __launch_bounds__(kMxThreads) mx_quantize_kernel(const T* __rest
   }
 }
 
-template <class T, bool WIDE>
+// The other way: a lane's eight codes are four bytes, what it writes 16 or 32.  LINEAR as above.  Bound: the values written.
+template <class T, bool WIDE, bool LINEAR>
 __global__ void __launch_bounds__(kMxThreads) mx_dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scale,
                                                                    int rows, int K, T* __restrict__ out, int64_t ld) {
   mx_dep_launch();
   mx_dep_wait();
   const int pitch = mx_pitch(K), per_row = (K + 255) >> 8, lane = threadIdx.x & 31;
-  const int64_t warp = ((int64_t)blockIdx.x * kMxThreads + threadIdx.x) >> 5;
-  MxRun run[kMxAhead];
-  mx_runs(warp * kMxAhead, rows, per_row, K, lane, run);
-  uint32_t w[kMxAhead], b[kMxAhead];
+  const int64_t runs = (int64_t)rows * per_row, step = (int64_t)gridDim.x * (kMxThreads / 32) * kMxAhead;
+  for (int64_t first = (((int64_t)blockIdx.x * kMxThreads + threadIdx.x) >> 5) * kMxAhead; first < runs; first += step) {
+    MxRun run[kMxAhead];
+    if constexpr (!LINEAR) mx_runs(first, rows, per_row, K, lane, run);
+    const int64_t at = first * 256 + lane * 8;
+    uint32_t w[kMxAhead], b[kMxAhead];
 #pragma unroll
-  for (int i = 0; i < kMxAhead; ++i) {
-    w[i] = b[i] = 0;
-    if (run[i].live) {
-      w[i] = __ldcg(reinterpret_cast<const uint32_t*>(codes + run[i].row * (K >> 1) + (run[i].c >> 1)));
-      b[i] = __ldcg(scale + run[i].row * pitch + run[i].c / kMxBlock);
+    for (int i = 0; i < kMxAhead; ++i) {
+      w[i] = b[i] = 0;
+      if constexpr (LINEAR) {
+        if (first + i < runs) {
+          w[i] = __ldcg(reinterpret_cast<const uint32_t*>(codes + (at >> 1) + 128 * i));
+          b[i] = __ldcg(scale + (at >> 5) + 8 * i);
+        }
+      } else if (run[i].live) {
+        w[i] = __ldcg(reinterpret_cast<const uint32_t*>(codes + run[i].row * (K >> 1) + (run[i].c >> 1)));
+        b[i] = __ldcg(scale + run[i].row * pitch + run[i].c / kMxBlock);
+      }
     }
-  }
 #pragma unroll
-  for (int i = 0; i < kMxAhead; ++i) {
-    if (!run[i].live) continue;
-    const float s = mx_scale_value(b[i]);
-    float v[8];
+    for (int i = 0; i < kMxAhead; ++i) {
+      if (LINEAR ? first + i >= runs : !run[i].live) continue;
+      const float s = mx_scale_value(b[i]);
+      float v[8];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float2 f = __half22float2(mx_decode2(w[i] >> (8 * j)));
-      v[2 * j] = f.x * s;
-      v[2 * j + 1] = f.y * s;
+      for (int j = 0; j < 4; ++j) {
+        const float2 f = __half22float2(mx_decode2(w[i] >> (8 * j)));
+        v[2 * j] = f.x * s;
+        v[2 * j + 1] = f.y * s;
+      }
+      if constexpr (LINEAR) mx_store8<T, WIDE>(out + at + 256 * i, v);
+      else mx_store8<T, WIDE>(out + run[i].row * ld + run[i].c, v);
     }
-    mx_store8<T, WIDE>(out + run[i].row * ld + run[i].c, v);
   }
 }
 
@@ -274,8 +284,8 @@ static int dequantize_as(const uint8_t* codes, const uint8_t* scale, int rows, i
   const bool wide = mx_aligned(out, 16) && (ld * sizeof(T)) % 16 == 0;
   const unsigned blocks = mx_run_blocks(rows, K);
   if (!blocks) return SLICEMOE_E_UNSUPPORTED;
-  return mx_launch(wide ? mx_dequantize_kernel<T, true> : mx_dequantize_kernel<T, false>, dim3(blocks), kMxThreads, 0,
-                   st, codes, scale, rows, K, static_cast<T*>(out), ld);
+  const auto kernel = wide && ld == K && K % 256 == 0 ? mx_dequantize_kernel<T, true, true> : wide ? mx_dequantize_kernel<T, true, false> : mx_dequantize_kernel<T, false, false>;
+  return mx_launch(kernel, dim3(blocks < 148 * 8 ? blocks : 148 * 8), kMxThreads, 0, st, codes, scale, rows, K, static_cast<T*>(out), ld);
 }
 
 static int mx_check(const void* x, int dtype, int rows, int K, int64_t ld, const void* codes, const void* scale) {
