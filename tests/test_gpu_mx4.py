@@ -122,7 +122,7 @@ class Case:
         self.T, self.k, self.E, self.N, self.K, self.gated, self.per_pair = T, k, E, N, K, gated, per_pair
         if per_pair:
             self.x = self.x.reshape(T, k, K)
-        self.ws = B.new_mx4_workspace(T, k, E)
+        self.ws = B.new_mx4_workspace(T, k, E, K)
 
     def dev(self):
         c, s = _t(self.c), _t(self.s)
@@ -145,7 +145,7 @@ class Case:
 @pytest.mark.parametrize("T,k,E,N,K", [
     (1, 1, 1, 1, 32), (1, 1, 1, 128, 64), (1, 6, 8, 100, 96), (1, 2, 4, 256, 2048), (3, 2, 5, 129, 160), (16, 4, 9, 64, 256), (17, 1, 1, 130, 416),
     (40, 3, 2, 200, 128), (224, 1, 1, 128, 128), (225, 1, 1, 128, 192), (300, 2, 3, 257, 288), (500, 2, 70, 48, 320), (2100, 4, 6, 32, 64), (5, 16, 40, 272, 1408),
-    (20, 3, 200, 32, 96), (400, 2, 1024, 16, 64), (4, 2, 1000, 48, 64)])
+    (20, 3, 200, 32, 96), (400, 2, 1024, 16, 64), (4, 2, 1000, 48, 64), (1, 2, 3, 40, 16384), (3, 2, 4, 24, 8192), (2, 1, 2, 20001, 64)])
 @pytest.mark.parametrize("gated", [False, True])
 def test_product_matches_the_oracle(T, k, E, N, K, gated):
     c = Case(T, k, E, N, K, gated)
