@@ -34,6 +34,7 @@ constexpr int kMpTile = 224, kMpLeastTile = 32;  // most tokens of a tile; of a 
 constexpr int kMpFew = 512;          // up to so many pairs, and
 constexpr int kMpResident = 96 * 1024;  // so many bytes of token rows, every CTA keeps all rows and plans for itself
 constexpr int kMpSortPairs = 4096;   // else: pairs of a block of the kernel that ranks them
+constexpr int kMpPlaceAll = 8192;    // pairs up to which the kernel that places them ranks them too
 constexpr int kMpSortThreads = 1024, kMpPlaceThreads = 256;
 
 // An expert's rows are cut into as few tiles as they fit, of equal size (a multiple of 16).
@@ -167,7 +168,7 @@ constexpr int kMpPlaceChunk = 128;
 struct MpPlace {
   uint32_t x, code, scale, row;  // row of x (all ones: none); rows, and blocks of scales, before the tile; rows of the tile << 16 | row in it
 };
-// FEW: no kernel has ranked the pairs; every block looks at all of them, which takes less than a launch up to kMpSortPairs, and takes 32
+// FEW: no kernel has ranked the pairs; every block looks at all of them, which takes less than a launch up to kMpPlaceAll, and takes 32
 // of them itself.  (300 tokens x 6: 5.8 us for two launches, and 2 to 3 of the 10 to 13 us of small calls.)
 template <bool FEW>
 __global__ void __launch_bounds__(FEW ? 2 * kMpPlaceThreads : kMpPlaceThreads, FEW ? 2 : 4) mp_place_kernel(const MpPlaceParams p) {
@@ -184,19 +185,21 @@ __global__ void __launch_bounds__(FEW ? 2 * kMpPlaceThreads : kMpPlaceThreads, F
   if constexpr (FEW) {
     __syncthreads();
     if (tid < 32 && base + tid < p.pairs) own = __ldcg(p.ids + base + tid);
-    constexpr int kAhead = kMpSortPairs / kThreads;
-    int id[kAhead];
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) id[i] = i * kThreads + tid < p.pairs ? __ldcg(p.ids + i * kThreads + tid) : -1;
+    constexpr int kAhead = 8;
     bool bad = false;
+    for (int i0 = tid; i0 < p.pairs; i0 += kAhead * kThreads) {
+      int id[kAhead];
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      const int at = i * kThreads + tid;
-      if ((unsigned)id[i] < (unsigned)p.E) {
-        atomicAdd(&s_count[id[i]], 1);
-        if (at < base) atomicAdd(&s_before[id[i]], 1);
-      } else {
-        bad |= at < p.pairs;
+      for (int i = 0; i < kAhead; ++i) id[i] = i0 + i * kThreads < p.pairs ? __ldcg(p.ids + i0 + i * kThreads) : -1;
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const int at = i0 + i * kThreads;
+        if ((unsigned)id[i] < (unsigned)p.E) {
+          atomicAdd(&s_count[id[i]], 1);
+          if (at < base) atomicAdd(&s_before[id[i]], 1);
+        } else {
+          bad |= at < p.pairs;
+        }
       }
     }
     if (bad && blockIdx.x == 0) atomicOr(&p.head->status, (unsigned)SLICEMOE_STATUS_BAD_EXPERT_ID);
@@ -969,7 +972,7 @@ extern "C" int slicemoe_mx4_product(const slicemoe_mx4_mat* mats, int n_experts,
   if (placed) {
     int *rank = reinterpret_cast<int*>(ws + l.rank), *hist = reinterpret_cast<int*>(ws + l.hist), *first = reinterpret_cast<int*>(ws + l.first),
         *list = reinterpret_cast<int*>(ws + l.list);
-    const bool few = ids && pairs <= kMpSortPairs;
+    const bool few = ids && pairs <= kMpPlaceAll;
     if (ids && !few) {
       const int rc = mx_launch(mp_sort_kernel, dim3(l.blocks), kMpSortThreads, 0, st, MpSortParams{ids, pairs, E, rank, hist, p.head});
       if (rc != SLICEMOE_OK) return rc;
