@@ -12,7 +12,7 @@
 //
 // Bound and measured (B200, in a graph): one token, gated, 6 experts of 1408 x 2048: 7.1 us, of which the weights' 18.4 MB take 2.8 at the
 // copy rate and the rest are latencies; 16 tokens 24 us, 77 tokens 36.6 us = 5.4 TB/s, the way from HBM; 2,048 tokens x 4 of 60, gated:
-// 57.5 us, HBM (184 MB of weights) and the placing of the rows; 8,192 x 6, 2048 x 1408: 124 us = 2.3 PFLOP/s, shared-memory bandwidth
+// 56 us, HBM (184 MB of weights) and the placing of the rows; 8,192 x 6, 2048 x 1408: 124 us = 2.3 PFLOP/s, shared-memory bandwidth
 // (47 KB come in and 44 KB are read a step, 700 clocks at 128 bytes a clock against 448 of products) and 20 us of placing.
 #include "decode_common.cuh"
 #include "mx4.cuh"
@@ -168,8 +168,9 @@ constexpr int kMpPlaceChunk = 128;
 struct MpPlace {
   uint32_t x, code, scale, row;  // row of x (all ones: none); rows, and blocks of scales, before the tile; rows of the tile << 16 | row in it
 };
-// FEW: no kernel has ranked the pairs; every block looks at all of them, which takes less than a launch up to kMpPlaceAll, and takes 32
-// of them itself.  (300 tokens x 6: 5.8 us for two launches, and 2 to 3 of the 10 to 13 us of small calls.)
+// FEW: no kernel has ranked the pairs; every block looks at all of them, which takes no longer than a launch up to kMpPlaceAll, and takes
+// 32 of them itself.  (300 tokens x 6: 3 us less than by two launches, like 2 to 3 of the 10 to 13 us of small calls.  2,048 x 4 of 60 experts of
+// 1408 x 2048, gated: 49.9 us so, 51.1 by two.  Further up it turns round: 16,384 tokens, 16 experts of 256 x 512: 29.8 us so, 21.6 by two.)
 template <bool FEW>
 __global__ void __launch_bounds__(FEW ? 2 * kMpPlaceThreads : kMpPlaceThreads, FEW ? 2 : 4) mp_place_kernel(const MpPlaceParams p) {
   constexpr int kThreads = FEW ? 2 * kMpPlaceThreads : kMpPlaceThreads, kRows = FEW ? 2 : 4;
