@@ -413,7 +413,7 @@ int slicemoe_prefill_layer(const slicemoe_shape *shape, const slicemoe_expert *e
  * Selection is that of exact arithmetic down to the rounding of 64-bit floats: where keys in 32 bits are too close to tell,
  * the token's keys are worked out again in 64.  Without a bias experts are ordered by their logits.
  * Errors: INVALID_ARG (null, T <= 0, k < 1, k > SLICEMOE_MAX_TOP_K, ld < E, E % n_group, topk_group not in [1, n_group],
- * group_best above a group's size, k > topk_group * E / n_group, logits off their type's alignment), UNSUPPORTED (E > 512,
+ * group_best above a group's size, k > topk_group * E / n_group, an array off its type's alignment), UNSUPPORTED (T > 2^30, E > 512,
  * n_group > 32, group_best not 1 or 2, an unknown dtype or score).
  */
 #define SLICEMOE_SCORE_SOFTMAX 0
@@ -435,7 +435,7 @@ int slicemoe_route_scored(const void *logits, int dtype, int T, int E, int64_t l
  * slicemoe_mx4_dequantize - the values again, into out [rows, K] of `dtype`, rows ld elements apart (bf16 and fp32 hold every value
  * exactly; fp16 rounds, and overflows beyond 65504).
  *   K % 32 == 0; codes 16-byte, scale 4-byte aligned; x and out aligned to their element type.
- * Errors: INVALID_ARG (null, rows <= 0, K <= 0, K % 32, ld < K, alignment), UNSUPPORTED (dtype; rows * ceil(K / 256) of 2^36 and more), CUDA.
+ * Errors: INVALID_ARG (null, rows <= 0, K <= 0, K % 32, ld < K, alignment), UNSUPPORTED (dtype; K > 2^30; rows * ceil(K / 256) of 2^36 and more), CUDA.
  */
 size_t slicemoe_mx4_scale_pitch(int K);
 int slicemoe_mx4_quantize(const void *x, int dtype, int rows, int K, int64_t ld, uint8_t *codes, uint8_t *scale, void *stream);
@@ -503,7 +503,7 @@ int slicemoe_mx4_product(const slicemoe_mx4_mat *mats, int n_experts, int N, int
  *   base       device [T, N] of out_dtype or NULL (a residual, or the shared experts' part); may be out itself
  *   out        device [T, N] of out_dtype
  * Arrays are aligned to their element type.  Errors: INVALID_ARG (null, T <= 0, N <= 0, k < 1, n_experts <= 0 with ids,
- * alignment), UNSUPPORTED (k > SLICEMOE_MAX_TOP_K, an unknown dtype), CUDA.
+ * alignment), UNSUPPORTED (k > SLICEMOE_MAX_TOP_K, N > 2^30, an unknown dtype), CUDA.
  */
 int slicemoe_combine(const void *rows, int rows_dtype, int T, int k, int N, const float *weights, const int32_t *ids,
                      int n_experts, const void *base, void *out, int out_dtype, void *stream);

@@ -465,6 +465,8 @@ class Mx4Table:
         self.N, self.K, self.gated, self.n_experts = first.N, first.K, first.gated, len(self.mats)
         arr = (Mx4MatDesc * len(self.mats))(*[m.desc() for m in self.mats])
         self.device_array = torch.frombuffer(bytearray(bytes(arr)), dtype=torch.uint8).to(device)
+        if any(t.device != self.device_array.device for m in self.mats for t in (m.codes, m.scale)):
+            raise ValueError("matrices on the table's device are wanted")
 
 
 def mx4_table(mats, device=None) -> Mx4Table:

@@ -104,7 +104,7 @@ __global__ void __launch_bounds__(kCbThreads, 3) combine_kernel(const CbParams p
       }
     } else {
       // two rows at a time
-      for (int j = 0; j < p.k; j += 2, row += 2 * p.N) {
+      for (int j = 0; j < p.k; j += 2, row += 2 * (int64_t)p.N) {
         float v[2][8], w[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -267,8 +267,9 @@ using namespace slicemoe;
 extern "C" int slicemoe_combine(const void* rows, int rows_dtype, int T, int k, int N, const float* weights, const int32_t* ids, int n_experts,
                                 const void* base, void* out, int out_dtype, void* stream) {
   if (!rows || !weights || !out || T <= 0 || k < 1 || N <= 0 || (ids && n_experts <= 0)) return SLICEMOE_E_INVALID_ARG;
-  if (k > SLICEMOE_MAX_TOP_K || !mx_dtype(rows_dtype) || !mx_dtype(out_dtype)) return SLICEMOE_E_UNSUPPORTED;
-  if (!mx_aligned(rows, mx_elem(rows_dtype)) || !mx_aligned(out, mx_elem(out_dtype)) || !mx_aligned(base, mx_elem(out_dtype)))
+  if (k > SLICEMOE_MAX_TOP_K || N > kMxMaxRow || !mx_dtype(rows_dtype) || !mx_dtype(out_dtype)) return SLICEMOE_E_UNSUPPORTED;
+  if (!mx_aligned(rows, mx_elem(rows_dtype)) || !mx_aligned(out, mx_elem(out_dtype)) || !mx_aligned(base, mx_elem(out_dtype)) || !mx_aligned(weights, 4) ||
+      !mx_aligned(ids, 4))
     return SLICEMOE_E_INVALID_ARG;
   const CbParams p = {rows, weights, ids, base, out, T, k, N, n_experts};
   cudaStream_t st = (cudaStream_t)stream;

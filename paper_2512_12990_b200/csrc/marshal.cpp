@@ -630,7 +630,7 @@ PyObject* py_route_scored(SM_ARGS) {
     }
     void* st = stream_of(a[12]);
     check(unlocked([&] {
-            return lib.route_scored(x.at, x.dtype, T, E, std::max(x.ld, x.cols), score, bias, n_group, topk_group, best, k, renorm, scale, tau,
+            return lib.route_scored(x.at, x.dtype, T, E, x.ld, score, bias, n_group, topk_group, best, k, renorm, scale, tau,
                                     rank_high, static_cast<int32_t*>(ids.data_ptr()), static_cast<float*>(w.data_ptr()),
                                     prec.defined() ? static_cast<uint8_t*>(prec.data_ptr()) : nullptr, st);
           }),

@@ -290,7 +290,7 @@ static int dequantize_as(const uint8_t* codes, const uint8_t* scale, int rows, i
 
 static int mx_check(const void* x, int dtype, int rows, int K, int64_t ld, const void* codes, const void* scale) {
   if (!x || !codes || !scale || rows <= 0 || K <= 0 || K % kMxBlock || ld < K) return SLICEMOE_E_INVALID_ARG;
-  if (!mx_dtype(dtype)) return SLICEMOE_E_UNSUPPORTED;
+  if (K > kMxMaxRow || !mx_dtype(dtype)) return SLICEMOE_E_UNSUPPORTED;
   if (!mx_aligned(x, mx_elem(dtype)) || !mx_aligned(codes, 16) || !mx_aligned(scale, 4)) return SLICEMOE_E_INVALID_ARG;
   return SLICEMOE_OK;
 }
@@ -299,7 +299,7 @@ static int mx_check(const void* x, int dtype, int rows, int K, int64_t ld, const
 
 using namespace slicemoe;
 
-extern "C" size_t slicemoe_mx4_scale_pitch(int K) { return K > 0 ? (size_t)mx_pitch(K) : 0; }
+extern "C" size_t slicemoe_mx4_scale_pitch(int K) { return K > 0 && K <= kMxMaxRow ? (size_t)mx_pitch(K) : 0; }
 
 extern "C" int slicemoe_mx4_quantize(const void* x, int dtype, int rows, int K, int64_t ld, uint8_t* codes, uint8_t* scale, void* stream) {
   const int rc = mx_check(x, dtype, rows, K, ld, codes, scale);

@@ -17,6 +17,7 @@ constexpr int kMxChunkBytes = kMxRows * kMxChunk / 2;
 constexpr int kMxAtomK = 128;   // values whose scales lie together
 constexpr int kMxAtomBytes = kMxRows * kMxAtomK / kMxBlock;
 constexpr int kMxMaxN = 1 << 21, kMxMaxK = 1 << 20;
+constexpr int kMxMaxRow = 1 << 30;  // values of a row, and rows, of the calls without matrices: counters that step past them stay within an int
 
 __host__ __device__ inline int mx_chunks(int K) { return (K + kMxChunk - 1) / kMxChunk; }
 __host__ __device__ inline int mx_atoms(int K) { return (K + kMxAtomK - 1) / kMxAtomK; }

@@ -493,10 +493,10 @@ extern "C" int slicemoe_route_scored(const void* logits, int dtype, int T, int E
                                      float* weights, uint8_t* prec_req, void* stream) {
   if (!logits || !ids || !weights || T <= 0 || E <= 0 || ld < E) return SLICEMOE_E_INVALID_ARG;
   if (k < 1 || k > SLICEMOE_MAX_TOP_K || n_group < 1 || E % n_group || topk_group < 1 || topk_group > n_group) return SLICEMOE_E_INVALID_ARG;
-  if (E > 512 || n_group > kRsMaxGroups || group_best < 1 || group_best > 2 || !mx_dtype(dtype)) return SLICEMOE_E_UNSUPPORTED;
+  if (T > kMxMaxRow || E > 512 || n_group > kRsMaxGroups || group_best < 1 || group_best > 2 || !mx_dtype(dtype)) return SLICEMOE_E_UNSUPPORTED;
   if (score != SLICEMOE_SCORE_SOFTMAX && score != SLICEMOE_SCORE_SIGMOID) return SLICEMOE_E_UNSUPPORTED;
   if (group_best > E / n_group || k > topk_group * (E / n_group)) return SLICEMOE_E_INVALID_ARG;
-  if (!mx_aligned(logits, mx_elem(dtype))) return SLICEMOE_E_INVALID_ARG;
+  if (!mx_aligned(logits, mx_elem(dtype)) || !mx_aligned(bias, 4) || !mx_aligned(ids, 4) || !mx_aligned(weights, 4)) return SLICEMOE_E_INVALID_ARG;
   RsParams p;
   p.logits = logits;
   p.ld = ld;

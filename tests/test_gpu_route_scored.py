@@ -130,3 +130,16 @@ def test_the_binding_refuses_what_does_not_fit():
             B.slicemoe_route_scored(bad, 2)
     with pytest.raises(B.SliceMoEError):
         B.slicemoe_route_scored(x, 65)
+
+
+def test_rows_that_overlap_are_refused():
+    """A broadcast row has no spacing: read as dense rows it would be read past its end."""
+    import torch
+    from paper_2512_12990_b200 import binding as B
+    x = torch.zeros(4 * 64, device="cuda")
+    for bad in (x[:64].expand(4, 64), x.as_strided((4, 64), (32, 1))):
+        with pytest.raises(B.SliceMoEError):
+            B.slicemoe_route_scored(bad, 2)
+        with pytest.raises(B.SliceMoEError):
+            B.slicemoe_mx4_quantize(bad)
+    B.slicemoe_route_scored(x[:64].expand(1, 64), 2)

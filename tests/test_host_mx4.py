@@ -119,3 +119,32 @@ def test_the_binding_wants_device_tensors():
         B.slicemoe_mx4_dequantize(torch.zeros((1, 32), dtype=torch.uint8), torch.zeros((1, 4), dtype=torch.uint8), torch.float32)
     with pytest.raises(TypeError):
         B.slicemoe_mx4_quantize([1.0])
+
+
+# Sizes that a kernel's counters would step past an int with, and arrays off their type's alignment.
+@pytest.mark.parametrize("kw,rc", [(dict(T=(1 << 30) + 1), -2), (dict(bias=p(4097)), -1), (dict(ids=p(4098)), -1), (dict(w=p(4097)), -1)])
+def test_route_refuses_long_lists_and_misaligned_arrays(kw, rc):
+    assert _route(**kw) == rc
+
+
+@pytest.mark.parametrize("call", ["slicemoe_mx4_quantize", "slicemoe_mx4_dequantize"])
+@pytest.mark.parametrize("K", [(1 << 30) + 32, (1 << 31) - 32])
+def test_quantize_refuses_longer_rows(call, K):
+    assert _quant(call, K=K, ld=K) == B.E_UNSUPPORTED
+    assert B.lib().slicemoe_mx4_scale_pitch(K) == 0
+
+
+@pytest.mark.parametrize("kw,rc", [(dict(N=(1 << 30) + 1), -2), (dict(N=(1 << 31) - 1), -2), (dict(w=p(4097)), -1), (dict(ids=p(4098), E=4), -1)])
+def test_combine_refuses_longer_rows_and_misaligned_arrays(kw, rc):
+    a = dict(rows=p(4096), rd=B.BF16, T=1, k=2, N=8, w=p(4096), ids=None, E=0, base=None, out=p(4096), od=B.BF16, stream=None)
+    a.update(kw)
+    assert B.lib().slicemoe_combine(*a.values()) == rc
+
+
+def test_a_table_wants_matrices_of_its_device():
+    import torch
+    at = {d: B.Mx4Mat(128, 64, False, torch.zeros(4096, dtype=torch.uint8, device=d), torch.zeros(512, dtype=torch.uint8, device=d)) for d in ("cpu", "meta")}
+    assert B.mx4_table([at["cpu"]]).n_experts == 1
+    for mats, device in (([at["cpu"], at["cpu"]], "meta"), ([at["cpu"], B.Mx4Mat(128, 64, False, at["cpu"].codes, at["meta"].scale)], "cpu")):
+        with pytest.raises(ValueError):
+            B.mx4_table(mats, device)
