@@ -376,7 +376,9 @@ __global__ void __launch_bounds__(32 * kRsWarps, VPT <= 8 ? 8 : 4) route_scored_
         const uint32_t low = __reduce_min_sync(0xffffffffu, kept ? order : 0xffffffffu), high = __reduce_max_sync(0xffffffffu, kept ? 0u : order);
         if (rs_near(rs_value(low), rs_value(high), 2.0f * near)) {  // the same in all lanes
           __syncwarp();
-          kept = real && ((rs_exact_keys<SIGMOID>(p, logits, s_bias, s_exact[warp], vmax, lane) >> me) & 1u);
+          // by all lanes, those without experts too: they exchange values in there
+          const uint32_t mask = rs_exact_keys<SIGMOID>(p, logits, s_bias, s_exact[warp], vmax, lane);
+          kept = real && ((mask >> me) & 1u);
         }
       }
       if (!kept) {

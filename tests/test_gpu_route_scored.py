@@ -143,3 +143,19 @@ def test_rows_that_overlap_are_refused():
         with pytest.raises(B.SliceMoEError):
             B.slicemoe_mx4_quantize(bad)
     B.slicemoe_route_scored(x[:64].expand(1, 64), 2)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("E,groups", [(4, 2), (16, 8), (32, 4), (48, 6), (96, 6), (160, 5), (320, 20), (480, 15)])
+def test_groups_that_32_bits_cannot_tell_apart_in_some_of_the_lanes(score, E, groups):
+    """Groups of whole lanes that leave lanes without experts, worth the same down to the rounding of a float32: told apart in 64 bits, by all
+    lanes of the warp together."""
+    rng = np.random.default_rng(E)
+    x = rng.normal(size=E).astype(np.float32)
+    p = 1.0 / (1.0 + np.exp(-x.astype(np.float64))) if score == "sigmoid" else np.exp(x.astype(np.float64)) / np.exp(x.astype(np.float64)).sum()
+    bias = (0.9 - p).astype(np.float32)
+    rows = np.tile(x, (60, 1))
+    rows[30:] += rng.normal(size=(30, E)).astype(np.float32) * 1e-6
+    for best in (1, 2):
+        for keep in {1, groups // 2, groups - 1}:
+            _check(rows, min(6, keep * (E // groups)), bias=bias, score=score, n_group=groups, topk_group=keep, group_best=best, renorm=True)
