@@ -20,8 +20,12 @@ namespace slicemoe {
 // below 0.6 x 2^-23 for every l; 1 + t rounds by 2^-24 s, __fdividef by 2 ulp, 2^-22 s; adding the bias by 2^-24 |key|: below
 // 2^-21.1 max(1, |key|), two keys 2^-20.1.  Softmax p = e^-d / sum: d rounds by 2^-24 d and d e^-d < 0.37; expf's 2 ulp and the sum's (16 terms
 // in a row, then 5 exchanges: at most 21 roundings of 2^-24, and expf's), the reciprocal and the product 2^-24 each: below 2^-18.9 p +
-// 0.37 x 2^-24, two keys 2^-17.8.  A group's value of two keys: twice that.
+// 0.37 x 2^-24, two keys 2^-17.8.
 constexpr float kNearSigmoid = 9.5367431640625e-7f, kNearSoftmax = 7.62939453125e-6f;  // 2^-20, 2^-17; times max(1, |key|)
+// A group's value: one key is off by less than half of that, 8 x 2^-24 max(1, |key|) and 64 x 2^-24, and a sum by its keys' errors and its own
+// rounding, both of which go with the keys and not with the sum: keys of opposite sign cancel, their errors do not.  kGroup holds them
+// and the rounding of the value's bounds.
+constexpr float kGroup = 0.625f;
 constexpr int kRsWarps = 4;
 constexpr int kRsMaxGroups = 32;
 
@@ -99,6 +103,14 @@ __device__ __forceinline__ bool rs_near(float a, float b, float near) {
   return !(a - b > near * fmaxf(1.0f, fmaxf(fabsf(a), fabsf(b)))) && !(isinf(a) && isinf(b));
 }
 
+// How far a group's value `v`, b0 or b0 + b1 if there are two, may be off.  One that is infinite is taken as it is.
+__device__ __forceinline__ float rs_group_error(float v, float b0, float b1, bool two, float near) {
+  const float size = fmaxf(1.0f, fabsf(b0)) + (two ? fmaxf(1.0f, fabsf(b1)) : 0.0f);
+  return isinf(v) ? 0.0f : kGroup * near * size;
+}
+// Whether the least that a kept group may be worth is above the most that a dropped one may be, or both are the same infinity.
+__device__ __forceinline__ bool rs_apart(float low, float high) { return low > high || (low == high && isinf(low)); }
+
 // Which groups are kept, as a bit mask, from the token's keys (of type F) in shared memory: `share` lanes scan a group each.
 template <class F>
 __device__ __forceinline__ uint32_t rs_groups(const RsParams& p, const F* keys, int lane, float near, bool* unsure) {
@@ -130,14 +142,15 @@ __device__ __forceinline__ uint32_t rs_groups(const RsParams& p, const F* keys, 
   }
   const bool counts = g < p.n_group && lane % share == 0, kept = counts && rank < p.topk_group;
   if (unsure) {
-    F low = kept ? mine : (F)CUDART_INF_F, high = counts && !kept ? mine : (F)-CUDART_INF_F;
+    const float v = (float)mine, err = rs_group_error(v, (float)b0, (float)b1, p.group_best == 2, near);
+    float low = kept ? v - err : CUDART_INF_F, high = counts && !kept ? v + err : -CUDART_INF_F;
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) {
-      const F l = __shfl_xor_sync(0xffffffffu, low, off), h = __shfl_xor_sync(0xffffffffu, high, off);
-      low = fmin(low, l);
-      high = fmax(high, h);
+      const float l = __shfl_xor_sync(0xffffffffu, low, off), h = __shfl_xor_sync(0xffffffffu, high, off);
+      low = fminf(low, l);
+      high = fmaxf(high, h);
     }
-    *unsure = p.topk_group < p.n_group && rs_near((float)low, (float)high, 2.0f * near);
+    *unsure = p.topk_group < p.n_group && !rs_apart(low, high);
   }
   const uint32_t lanes = __ballot_sync(0xffffffffu, kept);  // bit of group g from lane g * share
   uint32_t mask = 0;
@@ -356,15 +369,17 @@ __global__ void __launch_bounds__(32 * kRsWarps, VPT <= 8 ? 8 : 4) route_scored_
         b1 = max(min(b0, o0), max(b1, o1));
         b0 = max(b0, o0);
       }
-      float mine = rs_value(b0);
+      float first = rs_value(b0), second = 0.0f, mine = first;
       const bool sums = p.bias || p.group_best > 1;
       if (p.group_best > 1) {
-        const float second = rs_value(b1);
-        mine = p.bias ? mine + second : score(mine) + score(second);
+        second = rs_value(b1);
+        if (!p.bias) first = score(first), second = score(second);
+        mine = first + second;
+        if (isnan(mine)) mine = -CUDART_INF_F;
       }
       const int size = p.lanes, groups = p.n_group;
       const bool real = lane < groups * size;
-      const uint32_t order = real ? rs_ordered(isnan(mine) ? -CUDART_INF_F : mine) : 0u;
+      const uint32_t order = real ? rs_ordered(mine) : 0u;
       int rank = 0;
       const int me = lane / size;
       for (int o = 0; o < groups; ++o) {
@@ -373,8 +388,10 @@ __global__ void __launch_bounds__(32 * kRsWarps, VPT <= 8 ? 8 : 4) route_scored_
       }
       bool kept = real && rank < p.topk_group;
       if (sums && p.topk_group < groups) {
-        const uint32_t low = __reduce_min_sync(0xffffffffu, kept ? order : 0xffffffffu), high = __reduce_max_sync(0xffffffffu, kept ? 0u : order);
-        if (rs_near(rs_value(low), rs_value(high), 2.0f * near)) {  // the same in all lanes
+        const float err = rs_group_error(mine, first, second, p.group_best > 1, near);
+        const uint32_t low = __reduce_min_sync(0xffffffffu, kept ? rs_ordered(mine - err) : 0xffffffffu);
+        const uint32_t high = __reduce_max_sync(0xffffffffu, real && !kept ? rs_ordered(mine + err) : 0u);
+        if (!rs_apart(rs_value(low), rs_value(high))) {  // the same in all lanes
           __syncwarp();
           // by all lanes, those without experts too: they exchange values in there
           const uint32_t mask = rs_exact_keys<SIGMOID>(p, logits, s_bias, s_exact[warp], vmax, lane);

@@ -159,3 +159,18 @@ def test_groups_that_32_bits_cannot_tell_apart_in_some_of_the_lanes(score, E, gr
     for best in (1, 2):
         for keep in {1, groups // 2, groups - 1}:
             _check(rows, min(6, keep * (E // groups)), bias=bias, score=score, n_group=groups, topk_group=keep, group_best=best, renorm=True)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("E,groups", [(16, 8), (64, 4), (24, 8), (320, 20)])
+@pytest.mark.parametrize("size", [10.0, 300.0, 1e4, 1e6])
+def test_groups_whose_keys_cancel(score, E, groups, size):
+    """Biases of +size and -size in every group, in groups that share a number of lanes and in others: sums of about 1 whose error is that
+    of their keys.  The logits of a token are nearly alike, so that the sums differ by less than an fp32 rounding of a key."""
+    rng = np.random.default_rng(int(size) + E)
+    bias = np.full(E, -2 * size)
+    bias[::E // groups] = size
+    bias[1::E // groups] = -size
+    rows = rng.normal(size=(400, 1)) + rng.normal(size=(400, E)) * np.where(np.arange(400) % 2, 1e-5, 0.3)[:, None]
+    _check(rows.astype(np.float32), min(6, E // groups), bias=bias, score=score, n_group=groups,
+           topk_group=groups // 2, group_best=2, renorm=True)
