@@ -25,7 +25,7 @@ constexpr float kNearSigmoid = 9.5367431640625e-7f, kNearSoftmax = 7.62939453125
 // A group's value: one key is off by less than half of that, 8 x 2^-24 max(1, |key|) and 64 x 2^-24, and a sum by its keys' errors and its own
 // rounding, both of which go with the keys and not with the sum: keys of opposite sign cancel, their errors do not.  kGroup holds them
 // and the rounding of the value's bounds.
-constexpr float kGroup = 0.625f;
+constexpr float kGroup = 0.625f, kRsMaxFinite = 3.402823466e38f;
 constexpr int kRsWarps = 4;
 constexpr int kRsMaxGroups = 32;
 
@@ -103,13 +103,25 @@ __device__ __forceinline__ bool rs_near(float a, float b, float near) {
   return !(a - b > near * fmaxf(1.0f, fmaxf(fabsf(a), fabsf(b)))) && !(isinf(a) && isinf(b));
 }
 
-// How far a group's value `v`, b0 or b0 + b1 if there are two, may be off.  One that is infinite is taken as it is.
-__device__ __forceinline__ float rs_group_error(float v, float b0, float b1, bool two, float near) {
-  const float size = fmaxf(1.0f, fabsf(b0)) + (two ? fmaxf(1.0f, fabsf(b1)) : 0.0f);
-  return isinf(v) ? 0.0f : kGroup * near * size;
+// A group's value in 32 bits: its largest key, or half the sum of its two largest, which stays within the range of a float.
+__device__ __forceinline__ float rs_group_value(float b0, float b1, bool two) {
+  const float v = two ? 0.5f * b0 + 0.5f * b1 : b0;
+  return isnan(v) ? -CUDART_INF_F : v;
+}
+__device__ __forceinline__ double rs_group_value(double b0, double b1, bool two) {
+  const double v = two ? b0 + b1 : b0;
+  return isnan(v) ? -CUDART_INF : v;
+}
+// The least and the most that it may be worth.  An infinite one is taken as it is: a key is infinite, which no rounding has made it.  The
+// bounds of another are no infinities, even where they leave the range of a float.
+__device__ __forceinline__ void rs_group_bounds(float v, float b0, float b1, bool two, float near, float& least, float& most) {
+  const float far = kGroup * near, m0 = fmaxf(1.0f, fabsf(b0)), m1 = fmaxf(1.0f, fabsf(b1));
+  const float err = isinf(v) ? 0.0f : two ? 0.5f * far * m0 + 0.5f * far * m1 : far * m0, most_finite = isinf(v) ? CUDART_INF_F : kRsMaxFinite;
+  least = fmaxf(v - err, -most_finite);
+  most = fminf(v + err, most_finite);
 }
 // Whether the least that a kept group may be worth is above the most that a dropped one may be, or both are the same infinity.
-__device__ __forceinline__ bool rs_apart(float low, float high) { return low > high || (low == high && isinf(low)); }
+__device__ __forceinline__ bool rs_apart(float least, float most) { return least > most || (least == most && isinf(least)); }
 
 // Which groups are kept, as a bit mask, from the token's keys (of type F) in shared memory: `share` lanes scan a group each.
 template <class F>
@@ -133,8 +145,7 @@ __device__ __forceinline__ uint32_t rs_groups(const RsParams& p, const F* keys, 
     b1 = fmax(fmin(b0, o0), b0 >= o0 ? b1 : o1);
     b0 = fmax(b0, o0);
   }
-  F mine = p.group_best == 2 ? b0 + b1 : b0;
-  if (isnan(mine)) mine = (F)-CUDART_INF_F;
+  const F mine = rs_group_value(b0, b1, p.group_best == 2);
   int rank = 0;
   for (int o = 0; o < p.n_group; ++o) {
     const F v = __shfl_sync(0xffffffffu, mine, o * share);
@@ -142,8 +153,10 @@ __device__ __forceinline__ uint32_t rs_groups(const RsParams& p, const F* keys, 
   }
   const bool counts = g < p.n_group && lane % share == 0, kept = counts && rank < p.topk_group;
   if (unsure) {
-    const float v = (float)mine, err = rs_group_error(v, (float)b0, (float)b1, p.group_best == 2, near);
-    float low = kept ? v - err : CUDART_INF_F, high = counts && !kept ? v + err : -CUDART_INF_F;
+    float low, high;
+    rs_group_bounds((float)mine, (float)b0, (float)b1, p.group_best == 2, near, low, high);
+    if (!kept) low = CUDART_INF_F;
+    if (!counts || kept) high = -CUDART_INF_F;
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) {
       const float l = __shfl_xor_sync(0xffffffffu, low, off), h = __shfl_xor_sync(0xffffffffu, high, off);
@@ -369,14 +382,13 @@ __global__ void __launch_bounds__(32 * kRsWarps, VPT <= 8 ? 8 : 4) route_scored_
         b1 = max(min(b0, o0), max(b1, o1));
         b0 = max(b0, o0);
       }
-      float first = rs_value(b0), second = 0.0f, mine = first;
-      const bool sums = p.bias || p.group_best > 1;
-      if (p.group_best > 1) {
+      float first = rs_value(b0), second = 0.0f;
+      const bool sums = p.bias || p.group_best > 1, two = p.group_best > 1;
+      if (two) {
         second = rs_value(b1);
         if (!p.bias) first = score(first), second = score(second);
-        mine = first + second;
-        if (isnan(mine)) mine = -CUDART_INF_F;
       }
+      const float mine = rs_group_value(first, second, two);
       const int size = p.lanes, groups = p.n_group;
       const bool real = lane < groups * size;
       const uint32_t order = real ? rs_ordered(mine) : 0u;
@@ -388,9 +400,10 @@ __global__ void __launch_bounds__(32 * kRsWarps, VPT <= 8 ? 8 : 4) route_scored_
       }
       bool kept = real && rank < p.topk_group;
       if (sums && p.topk_group < groups) {
-        const float err = rs_group_error(mine, first, second, p.group_best > 1, near);
-        const uint32_t low = __reduce_min_sync(0xffffffffu, kept ? rs_ordered(mine - err) : 0xffffffffu);
-        const uint32_t high = __reduce_max_sync(0xffffffffu, real && !kept ? rs_ordered(mine + err) : 0u);
+        float least, most;
+        rs_group_bounds(mine, first, second, two, near, least, most);
+        const uint32_t low = __reduce_min_sync(0xffffffffu, kept ? rs_ordered(least) : 0xffffffffu);
+        const uint32_t high = __reduce_max_sync(0xffffffffu, real && !kept ? rs_ordered(most) : 0u);
         if (!rs_apart(rs_value(low), rs_value(high))) {  // the same in all lanes
           __syncwarp();
           // by all lanes, those without experts too: they exchange values in there

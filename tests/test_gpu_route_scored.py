@@ -174,3 +174,19 @@ def test_groups_whose_keys_cancel(score, E, groups, size):
     rows = rng.normal(size=(400, 1)) + rng.normal(size=(400, E)) * np.where(np.arange(400) % 2, 1e-5, 0.3)[:, None]
     _check(rows.astype(np.float32), min(6, E // groups), bias=bias, score=score, n_group=groups,
            topk_group=groups // 2, group_best=2, renorm=True)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("E,groups", [(16, 8), (64, 4), (24, 8)])
+def test_groups_whose_sums_leave_the_range_of_fp32(score, E, groups):
+    """Groups masked with the lowest float, or near it, are worth less than any other and more than one masked with -inf."""
+    rng = np.random.default_rng(E)
+    size, low = E // groups, float(np.finfo(np.float32).min)
+    x = rng.normal(size=(20, E)).astype(np.float32)
+    for worth in ([0, 0, -np.inf, low], [low, -np.inf, 0, 0], [-np.inf, low, -3e38, 0], [low, -3e38, -1.8e38, -np.inf]):
+        bias = np.repeat(np.array(worth + [-np.inf] * (groups - 4)), size)
+        for keep in range(1, groups):
+            _check(x, min(16, keep * size), bias=bias, score=score, n_group=groups, topk_group=keep, group_best=2)
+    bias = np.repeat(np.array([3e38, -low, -low, 0] + [-np.inf] * (groups - 4)), size)
+    for keep in (1, 2, 3):
+        _check(x, min(16, keep * size), bias=bias, score=score, n_group=groups, topk_group=keep, group_best=2)
