@@ -406,7 +406,7 @@ int slicemoe_prefill_layer(const slicemoe_shape *shape, const slicemoe_expert *e
  *              sum of its group_best (1 or 2) largest keys; only experts of the topk_group groups of largest value are
  *              selected.  n_group = 1: no groups
  *   k          experts per token, by descending key.  Ties, of groups too, go to the lower index
- *   renorm     1: the k scores are divided by their sum (weights are 0 where the sum is)
+ *   renorm     1: the k scores are divided by their sum, also where fp32 does not hold them (weights are 0 where the sum is 0 in 64 bits)
  *   scale      a factor of the weights, applied last
  *   tau, rank_high, prec_req   as in slicemoe_route_topk, on the score before renorm and scale
  *   ids        device int32 [T, k]; weights device float32 [T, k]; prec_req device uint8 [T, k] or NULL

@@ -25,7 +25,7 @@ constexpr float kNearSigmoid = 9.5367431640625e-7f, kNearSoftmax = 7.62939453125
 // A group's value: one key is off by less than half of that, 8 x 2^-24 max(1, |key|) and 64 x 2^-24, and a sum by its keys' errors and its own
 // rounding, both of which go with the keys and not with the sum: keys of opposite sign cancel, their errors do not.  kGroup holds them
 // and the rounding of the value's bounds.
-constexpr float kGroup = 0.625f, kRsMaxFinite = 3.402823466e38f;
+constexpr float kGroup = 0.625f, kRsMaxFinite = 3.402823466e38f, kRsLeast = 1.17549435e-38f;
 constexpr int kRsWarps = 4;
 constexpr int kRsMaxGroups = 32;
 
@@ -218,6 +218,16 @@ __device__ __noinline__ int rs_reorder(const RsParams& p, const float* logits, c
     if (r == lane) mine = i;
   }
   return mine;
+}
+
+// The share of the first k lanes' logits' scores in their sum, in 64 bits; a score that those do not hold either is 0.
+template <bool SIGMOID>
+__device__ __noinline__ float rs_share(const RsParams& p, const float* logits, float vmax, float l, int lane) {
+  const double total = rs_total<SIGMOID>(p, logits, vmax, lane), s = lane < p.k ? rs_score<SIGMOID>(l, vmax, total) : 0.0;
+  double sum = s;
+#pragma unroll 1
+  for (int off = 8; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+  return sum > 0.0 ? (float)(s / sum) : 0.0f;
 }
 
 // A token's keys in 64 bits, and which groups are kept by them, as a bit mask.
@@ -490,6 +500,8 @@ __global__ void __launch_bounds__(32 * kRsWarps, VPT <= 8 ? 8 : 4) route_scored_
 #pragma unroll
       for (int off = 8; off > 0; off >>= 1) total += __shfl_xor_sync(0xffffffffu, total, off);
       w = total > 0.0f ? s / total : 0.0f;
+      // a score that fp32 does not hold, in a sum that does not outweigh it: the quotients in 64 bits
+      if (__any_sync(0xffffffffu, lane < p.k && s < kRsLeast && total < 0.25f && l > -CUDART_INF_F)) w = rs_share<SIGMOID>(p, logits, vmax, l, lane);
     }
     if (lane < p.k) {
       const int64_t o = (int64_t)t * p.k + lane;

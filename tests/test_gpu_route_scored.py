@@ -190,3 +190,24 @@ def test_groups_whose_sums_leave_the_range_of_fp32(score, E, groups):
     bias = np.repeat(np.array([3e38, -low, -low, 0] + [-np.inf] * (groups - 4)), size)
     for keep in (1, 2, 3):
         _check(x, min(16, keep * size), bias=bias, score=score, n_group=groups, topk_group=keep, group_best=2)
+
+
+@pytest.mark.parametrize("groups", [1, 4])
+def test_scores_below_the_range_of_fp32_are_renormalised(groups):
+    """The weights are ratios of scores: that the scores themselves are below what fp32 holds does not make them 0."""
+    rng = np.random.default_rng(11)
+    x = rng.normal(size=(12, 64)).astype(np.float32) - np.array([80, 87, 88, 89, 95, 103, 104, 150, 300, 600, 87.5, 100], np.float32)[:, None]
+    x[10] -= np.arange(64, dtype=np.float32)
+    x[11, ::5] = -np.inf
+    kw = dict(n_group=groups, topk_group=min(groups, 2), renorm=True, scale=2.5)
+    for dtype in ("f32", "bf16", "f16"):
+        for bias in (None, rng.normal(size=64) * 0.1):
+            _check(x, 6, dtype, bias, score="sigmoid", **kw)
+    y = rng.normal(size=(12, 64)).astype(np.float32)                # experts that no token is to take, far above the others
+    y[:, [3, 17, 40]] += np.array([50, 80, 87, 88, 95, 103, 104, 150, 300, 600, 87.5, 100], np.float32)[:, None]
+    y[10] -= np.arange(64, dtype=np.float32)
+    bias = rng.normal(size=64) * 0.1
+    for mask in (-np.inf, -1e9):
+        bias[[3, 17, 40]] = mask
+        for dtype in ("f32", "f16"):
+            _check(y, 6, dtype, bias, score="softmax", **kw)
