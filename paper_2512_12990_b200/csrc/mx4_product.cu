@@ -451,7 +451,8 @@ __global__ void __launch_bounds__(kMpThreads, 1) mp_product_kernel(const MpParam
   } else if (warp == kMpPlanWarp) {
     if (lane == 0) {
       s->dead = 0;
-      s->limit = p.head->wait_cycles ? p.head->wait_cycles : kWaitCycles;
+      const unsigned long long cycles = __ldcg(&p.head->wait_cycles);
+      s->limit = cycles ? cycles : kWaitCycles;
     }
   } else if (warp >= kMpFirstDrain && warp < kMpFirstDrain + 2) {
     // one barrier to a thread: they lie one behind the other in the order of MpSmem
@@ -632,11 +633,9 @@ __global__ void __launch_bounds__(kMpThreads, 1) mp_product_kernel(const MpParam
       uint32_t slot = 0, turn = 0, st = 0, head = 0;
       uint32_t live = 0, old = 0, old_ph = 0;  // steps not known to be consumed, the oldest one's barrier
       uint32_t filled = 0;
-      const bool bring = p.head->extra_arrivals == 0;
-      if constexpr (PLACED) {
-        mx_dep_wait();
-        asm volatile("fence.proxy.async;" ::: "memory");  // the tiles were written by ordinary stores
-      }
+      mx_dep_wait();  // first of all, like every role: the time that the kernel before still takes does not count against the waits' limit
+      const bool bring = __ldcg(&p.head->extra_arrivals) == 0;
+      if constexpr (PLACED) asm volatile("fence.proxy.async;" ::: "memory");  // the tiles were written by ordinary stores
       bool ok = true;
       while (ok && (ok = mbar_wait(smem_u32(&s->item_known[slot]), turn, &s->dead, status))) {
         const MpItem item = s->item[slot];
@@ -694,6 +693,7 @@ __global__ void __launch_bounds__(kMpThreads, 1) mp_product_kernel(const MpParam
     // than the weights take to arrive; 285 with warp-wide waits.) ----
     if (mp_elect()) {
       uint32_t slot = 0, turn = 0, st = 0, ph = 0, acc = 0, acc_ph = 0, flip = 0, head = 0;
+      mx_dep_wait();
       bool ok = PLACED || mbar_wait(smem_u32(&s->resident), 0, &s->dead, status);
       while (ok && (ok = mbar_wait(smem_u32(&s->item_known[slot]), turn, &s->dead, status))) {
         const int n = s->item[slot].n, rows = s->item[slot].rows;

@@ -125,3 +125,27 @@ def test_the_product_of_microscaled_experts_gives_up_by_itself(T):
     B.slicemoe_workspace_set_wait(ws, 0, 0)
     assert torch.equal(B.slicemoe_mx4_product(table, codes, scale, ids, ws, dtype=torch.float32), ref)
     assert B.slicemoe_get_status(ws) == 0
+
+
+@pytest.mark.parametrize("T,k", [(2, 2), (40, 2), (260, 2), (5000, 2)])
+def test_a_short_limit_of_the_product_is_not_spent_on_the_launch_before(T, k):
+    """The product starts while the kernel before it still runs - here one of one block that goes through 2^20 values of K, longer
+    than the limit, and lets the next start at once.  Its waits are counted from the end of that: a limit of 200,000 cycles, 100 us, lets it
+    through.  (Rows resident in shared memory, planned by a warp or by all; placed by one kernel, by two.)"""
+    import torch
+    from paper_2512_12990_b200 import binding as B
+    E, N, K, far = 4, 256, 512, 1 << 20
+    long_table = B.mx4_table([B.slicemoe_mx4_pack(torch.randn(16, far, device="cuda"))])
+    long_x, long_ws = B.slicemoe_mx4_quantize(torch.randn(1, far, device="cuda")), B.new_mx4_workspace(1, 1, 1, far)
+    table, ws = B.mx4_table([B.slicemoe_mx4_pack(torch.randn(N, K, device="cuda")) for _ in range(E)]), B.new_mx4_workspace(T, k, E, K)
+    x = B.slicemoe_mx4_quantize(torch.randn(T, K, device="cuda"))
+    ids = torch.randint(0, E, (T, k), device="cuda", dtype=torch.int32)
+    want = B.slicemoe_mx4_product(table, *x, ids, ws, dtype=torch.float32)
+    first = B.slicemoe_mx4_product(long_table, *long_x, None, long_ws, dtype=torch.float32)
+    B.slicemoe_workspace_set_wait(ws, 200_000)
+    torch.cuda.synchronize()
+    for _ in range(5):
+        again = B.slicemoe_mx4_product(long_table, *long_x, None, long_ws, dtype=torch.float32)
+        out = B.slicemoe_mx4_product(table, *x, ids, ws, dtype=torch.float32)
+        assert torch.equal(out, want) and torch.equal(again, first)
+    assert B.slicemoe_get_status(ws) == 0 and B.slicemoe_get_status(long_ws) == 0
