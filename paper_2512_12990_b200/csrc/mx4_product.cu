@@ -340,7 +340,7 @@ struct __align__(16) MpSmem {
 static_assert(offsetof(MpSmem, pair) % 16 == 0 && kMpTile % 4 == 0 && offsetof(MpSmem, mats) % 8 == 0, "alignment");
 static_assert(offsetof(MpSmem, limit) == offsetof(MpSmem, dead) + 8, "wait_limit()");
 constexpr int kMpFixed = (int)((sizeof(MpSmem) + 1023) / 1024 * 1024);
-constexpr int kMpSmemMax = 227 * 1024, kMpSmemMin = 116 * 1024;  // one CTA to an SM: each takes all of tensor memory
+constexpr int kMpSmem = 227 * 1024;  // all of it, whatever the call: one CTA to an SM, since each takes all of tensor memory
 
 // A step in the ring: weights, their scales, token rows, their scales.  Steps lie one behind the other, each as long as its item's
 // tile needs, and start again at 0 where the next does not fit: who fills and who reads work out the same places.
@@ -897,12 +897,10 @@ static int mp_launch(const MpParams& p, int ctas, cudaStream_t st) {
   int dev = 0;
   SM_CUDA_TRY(cudaGetDevice(&dev));
   if (!attr_set[dev]) {  // mp_sm_count() has looked at the device's number
-    SM_CUDA_TRY(cudaFuncSetAttribute(mp_product_kernel<O, GATED, PLACED>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMpSmemMax));
+    SM_CUDA_TRY(cudaFuncSetAttribute(mp_product_kernel<O, GATED, PLACED>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMpSmem));
     attr_set[dev] = true;
   }
-  const int smem = kMpFixed + p.resident + p.ring;
-  return mx_launch(mp_product_kernel<O, GATED, PLACED>, dim3(ctas), kMpThreads,
-                   (size_t)(smem > kMpSmemMin ? smem : kMpSmemMin), st, MpParams(p));
+  return mx_launch(mp_product_kernel<O, GATED, PLACED>, dim3(ctas), kMpThreads, (size_t)kMpSmem, st, MpParams(p));
 }
 template <class O>
 static int mp_launch_as(const MpParams& p, int ctas, cudaStream_t st) {
@@ -965,7 +963,7 @@ extern "C" int slicemoe_mx4_product(const slicemoe_mx4_mat* mats, int n_experts,
   p.row_blocks = mx_row_blocks(N, gated);
   p.tile = placed ? mp_tile(T, pairs, E, p.row_blocks, sms) : rows16;
   p.resident = placed ? 0 : (int)((held + 1023) & ~1023);
-  p.ring = kMpSmemMax - kMpFixed - p.resident;
+  p.ring = kMpSmem - kMpFixed - p.resident;
   p.stages = kMpMaxStages;
   if (!placed && p.stages > p.ring / (kMpABytes + kMpAScaleBytes)) p.stages = p.ring / (kMpABytes + kMpAScaleBytes);
   const int64_t tiles = placed ? (int64_t)pairs / p.tile + (pairs < E ? pairs : E) : pairs, items = tiles * p.row_blocks;
