@@ -476,3 +476,34 @@ def test_long_prompts_agree_with_single_rows(T, k, E, N, K, dtype):
         tol = K * 2.0 ** -23 * (1.1 * u.abs() * mg + torch.nn.functional.silu(g).abs() * mu) + 2.0 ** -20 * y.abs()
         tol = tol + torch.from_numpy(np.asarray(_half_step((y.abs() + tol).cpu().numpy(), dtype))).cuda()
         assert ((out[at[:, 0], at[:, 1]].double() - y).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("T,k,E,N,K", [(1, 1, 1, 40, 16384), (3, 2, 4, 24, 16384), (16, 2, 3, 130, 8192), (300, 2, 3, 72, 4160), (230, 1, 2, 40, 16384),
+                                       (3, 2, 3, 129, 2048), (700, 3, 5, 64, 992)])
+def test_sums_that_fp32_holds_exactly_come_out_exact(T, k, E, N, K):
+    """Every block's scale is 1: a product of two values is a whole number of quarters, 144 of them at most, and K of them stay below 2^24
+    quarters.  Whatever the order, no sum is rounded: the result is that of whole numbers, and a block of K that is skipped, doubled or scaled
+    wrongly anywhere shows."""
+    import torch
+    from paper_2512_12990_b200 import binding as B
+    assert K * 144 < 2 ** 24
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(T + K)
+    grid = torch.tensor(np.concatenate([mx4.VALUES, -mx4.VALUES]), device="cuda")
+
+    def values(rows):                                # the first of a block 4, 6, -4 or -6: exponent 2, scale 1
+        c = torch.randint(0, 16, (rows, K // 32, 32), device="cuda", generator=gen)
+        c[:, :, 0] = (c[:, :, 0] & 9) | 6
+        return grid[c].reshape(rows, K)
+
+    x, w = values(T), [values(N) for _ in range(E)]
+    codes, scale = B.slicemoe_mx4_quantize(x.float())
+    assert (scale[:, :K // 32] == 127).all() and torch.equal(B.slicemoe_mx4_dequantize(codes, scale, torch.float32).double(), x)
+    table = B.mx4_table([B.slicemoe_mx4_pack(m.float()) for m in w])
+    ids = torch.randint(0, E, (T, k), device="cuda", generator=gen, dtype=torch.int32)
+    out = B.slicemoe_mx4_product(table, codes, scale, ids, B.new_mx4_workspace(T, k, E, K), dtype=torch.float32)
+    want = torch.empty((T, k, N), dtype=torch.float64, device="cuda")
+    for e in range(E):
+        at = torch.nonzero(ids == e)
+        want[at[:, 0], at[:, 1]] = x[at[:, 0]] @ w[e].T
+    assert torch.equal(out.double(), want)
