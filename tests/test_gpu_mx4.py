@@ -507,3 +507,79 @@ def test_sums_that_fp32_holds_exactly_come_out_exact(T, k, E, N, K):
         at = torch.nonzero(ids == e)
         want[at[:, 0], at[:, 1]] = x[at[:, 0]] @ w[e].T
     assert torch.equal(out.double(), want)
+
+
+# ---- long lists and large arrays -----------------------------------------------------------------------------------
+@pytest.mark.parametrize("T,k,E,listed", [(16384, 8, 16, True), (30000, 1, 5, True), (20000, 3, 300, True), (70000, 16, 64, True), (130000, 1, 1, False)])
+def test_lists_of_many_pairs(T, k, E, listed):
+    """Up to a million pairs: blocks of the kernels ahead take 64, 128 and more of them, in more than one go.  Sums are whole numbers of
+    quarters, so that every value is known exactly."""
+    import torch
+    from paper_2512_12990_b200 import binding as B
+    N, K = 24, 64
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(T)
+    grid = torch.tensor(np.concatenate([mx4.VALUES, -mx4.VALUES]), device="cuda")
+
+    def values(rows):
+        c = torch.randint(0, 16, (rows, K // 32, 32), device="cuda", generator=gen)
+        c[:, :, 0] = (c[:, :, 0] & 9) | 6
+        return grid[c].reshape(rows, K)
+
+    x, w = values(T), torch.stack([values(N) for _ in range(E)])
+    codes, scale = B.slicemoe_mx4_quantize(x.float())
+    table, ws = B.mx4_table([B.slicemoe_mx4_pack(m.float()) for m in w]), B.new_mx4_workspace(T, k, E, K)
+    ids = torch.randint(0, E, (T, k), device="cuda", generator=gen, dtype=torch.int32) if listed else torch.zeros((T, 1), device="cuda", dtype=torch.int32)
+    if listed:
+        ids[::97, 0] = -1
+    out = torch.full((T, k, N) if listed else (T, N), 77.0, device="cuda")
+    B.slicemoe_mx4_product(table, codes, scale, ids if listed else None, ws, out=out)
+    out = out.view(T, k, N)
+    for e in range(E):
+        at = torch.nonzero(ids == e)
+        assert torch.equal(out[at[:, 0], at[:, 1]].double(), x[at[:, 0]] @ w[e].T)
+    assert (out[ids < 0] == 77).all() and B.slicemoe_get_status(ws) == (B.STATUS_BAD_EXPERT_ID if listed else 0)
+
+
+def test_arrays_of_more_than_2_31_elements():
+    """Results, codes, rows and spacings whose places pass 32 bits: what lies at their ends against calls of those rows alone."""
+    import torch
+    from paper_2512_12990_b200 import binding as B
+    # quantise and back: 4.3e9 values, 2.1e9 bytes of codes
+    rows, K = 70000, 61440
+    x = torch.empty((rows, K), device="cuda", dtype=torch.bfloat16).normal_()
+    codes, scale = B.slicemoe_mx4_quantize(x)
+    back = B.slicemoe_mx4_dequantize(codes, scale, torch.bfloat16)
+    assert codes.numel() > 2 ** 31 and x.numel() > 2 ** 32
+    for at in (slice(0, 3), slice(34949, 34955), slice(69899, 69906), slice(rows - 4, rows)):    # 2^31 values: row 34,952; 2^32: row 69,905
+        c, s = B.slicemoe_mx4_quantize(x[at].contiguous())
+        assert torch.equal(codes[at], c) and torch.equal(scale[at], s)
+        assert torch.equal(back[at], B.slicemoe_mx4_dequantize(c, s, torch.bfloat16))
+    del back, codes, scale
+    # rows 2^31 and more elements apart
+    wide = x.view(-1)[:2 ** 32].view(2, 2 ** 31)
+    for off in (0, 5):
+        part = wide[:, off:off + 256]
+        want = part.contiguous()
+        assert all(torch.equal(a, b) for a, b in zip(B.slicemoe_mx4_quantize(part), B.slicemoe_mx4_quantize(want)))
+        assert all(torch.equal(a, b) for a, b in zip(B.slicemoe_route_scored(part, 8, score="sigmoid"), B.slicemoe_route_scored(want, 8, score="sigmoid")))
+    # combine: 4.3e9 values in
+    T, k, N = 70000, 4, 15360
+    big, w = x.view(T, k, N), torch.randn(T, k, device="cuda")
+    y = B.slicemoe_combine(big, w, dtype=torch.bfloat16)
+    odd = B.slicemoe_combine(x.view(-1)[1:1 + (T - 1) * k * N].view(T - 1, k, N), w[1:].contiguous(), dtype=torch.float32)    # off 16 bytes
+    for at in (slice(0, 3), slice(34949, 34955), slice(69899, 69906), slice(T - 4, T - 1)):
+        assert torch.equal(y[at], B.slicemoe_combine(big[at].contiguous(), w[at].contiguous(), dtype=torch.bfloat16))
+        rows_at = x.view(-1)[1 + at.start * k * N:1 + at.stop * k * N].clone().view(-1, k, N)
+        assert torch.equal(odd[at], B.slicemoe_combine(rows_at, w[1:][at].contiguous(), dtype=torch.float32))
+    del x, big, y, odd, wide, part
+    # product: 2.4e9 results
+    T, k, E, N, K = 18000, 8, 2, 16384 + 200, 96
+    table = B.mx4_table([B.slicemoe_mx4_pack(torch.randn(N, K, device="cuda")) for _ in range(E)])
+    codes, scale = B.slicemoe_mx4_quantize(torch.randn(T, K, device="cuda"))
+    ids, ws = torch.randint(0, E, (T, k), device="cuda", dtype=torch.int32), B.new_mx4_workspace(T, k, E, K)
+    out = B.slicemoe_mx4_product(table, codes, scale, ids, ws, dtype=torch.bfloat16)
+    assert out.numel() > 2 ** 31 and B.slicemoe_get_status(ws) == 0
+    for at in (slice(0, 3), slice(16184, 16190), slice(T - 3, T)):     # 2^31 values: token 16,187
+        one = B.slicemoe_mx4_product(table, codes[at].contiguous(), scale[at].contiguous(), ids[at].contiguous(), ws, dtype=torch.bfloat16)
+        assert torch.equal(out[at], one)
