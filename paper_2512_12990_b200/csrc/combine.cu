@@ -132,8 +132,8 @@ __global__ void __launch_bounds__(kCbThreads, 3) combine_kernel(const CbParams p
 }
 
 // The same for 16-bit rows that come from HBM: what a lane needs of the next two runs is on its way into shared memory (its own 16 bytes of every
-// row and of the base, so that no lane waits for another) while one is added up.  Registers hold one run's rows at most, 74 KB an SM, and
-// a block that ends takes its place with it: 53 us for 8,192 tokens x 6 of 2,048, 5.0 TB/s.
+// row and of the base, so that no lane waits for another) while one is added up: 48 us for 8,192 tokens x 6 of 2,048, 5.6 TB/s.  (The kernel
+// above takes 53: its registers hold one run's rows at most, 74 KB an SM, and a block that ends takes its place with it.)
 constexpr int kCbDepth = 3, kCbMostRows = 8, kCbSmem = 113 * 1024;
 constexpr int64_t kCbStreamBytes = 112 << 20;
 __host__ __device__ constexpr int cb_slot(int k, int base_bytes) { return k * 16 + base_bytes; }  // of a lane and a run

@@ -10,10 +10,13 @@
 // Sums are fp32 in tensor memory and rounded once.  Which column of a tile a token has does not enter its sum, so a row's
 // result does not depend on the rest of the call.
 //
-// Bound and measured (B200, in a graph): one token, gated, 6 experts of 1408 x 2048: 7.1 us, of which the weights' 18.4 MB take 2.8 at the
-// copy rate and the rest are latencies; 16 tokens 24 us, 77 tokens 36.6 us = 5.4 TB/s, the way from HBM; 2,048 tokens x 4 of 60, gated:
-// 56 us, HBM (184 MB of weights) and the placing of the rows; 8,192 x 6, 2048 x 1408: 124 us = 2.3 PFLOP/s, shared-memory bandwidth
-// (47 KB come in and 44 KB are read a step, 700 clocks at 128 bytes a clock against 448 of products) and 20 us of placing.
+// Bound and measured (B200, in a graph).  One token, gated, 6 experts of 1408 x 2048: 7.4 us where the weights come from HBM, 6.1 where L2
+// still holds them; their 18.4 MB take 2.8 at the copy rate, the rest are latencies.  16 tokens that name 39 experts (119 MB): 24.3 us =
+// 4.9 TB/s, and 22.2 from L2: 5.8 items to a CTA, so that some end early.  64 tokens, 59 experts: 33.6 us = 5.4 TB/s, the way from HBM.  2,048
+// tokens x 4 of 60, gated: 56 us, HBM (184 MB of weights), the placing of the rows ahead, and ramp and tail.  8,192 x 6, 2048 x 1408: 125 us =
+// 2.3 PFLOP/s (140 where it goes on for tenths of a second, at the power limit's clocks): 20 us of placing, and the drain.  An item of 224
+// tokens is 5.5 steps of 711 clocks of shared-memory traffic (47 KB come in and 44 KB are read at 128 bytes a clock; its products take 448), 3,900,
+// which the drain's exchanges and 4-byte stores, on the same way, are longer than.
 #include "decode_common.cuh"
 #include "mx4.cuh"
 
@@ -168,9 +171,14 @@ constexpr int kMpPlaceChunk = 128;
 struct MpPlace {
   uint32_t x, code, scale, row;  // row of x (all ones: none); rows, and blocks of scales, before the tile; rows of the tile << 16 | row in it
 };
-// FEW: no kernel has ranked the pairs; every block looks at all of them, which takes no longer than a launch up to kMpPlaceAll, and takes
-// 32 of them itself.  (300 tokens x 6: 3 us less than by two launches, like 2 to 3 of the 10 to 13 us of small calls.  2,048 x 4 of 60 experts of
-// 1408 x 2048, gated: 49.9 us so, 51.1 by two.  Further up it turns round: 16,384 tokens, 16 experts of 256 x 512: 29.8 us so, 21.6 by two.)
+// FEW: no kernel has ranked the pairs; every block looks at all of them and takes 32 of them itself, which saves a launch.  That pays while all
+// blocks are resident together, two to an SM: 296 of them, 9,472 pairs.  Products in a graph, so / by two launches, in us:
+//   pairs                               1,024          4,096          8,192          10,240         16,384
+//   16 experts, 256 x 512            8.1 /  9.1    10.0 / 10.8    12.2 / 12.7    16.9 / 13.5    25.3 / 17.3
+//   64 experts, 256 x 256            8.7 /  9.3    11.3 / 12.0    13.7 / 14.2    19.0 / 15.4    24.7 / 16.5
+//   60 experts, gated 1408 x 2048   38.8 / 41.7    42.6 / 45.3    49.2 / 51.7    60.1 / 57.4    86.5 / 78.9
+//   64 experts, 2048 x 1408         26.0 / 29.5    29.1 / 33.1    35.7 / 37.8    44.5 / 41.3    63.3 / 56.1
+//   256 experts, 512 x 2048         34.8 / 37.3    36.7 / 39.8    40.1 / 42.2    46.7 / 43.5    53.9 / 46.1
 template <bool FEW>
 __global__ void __launch_bounds__(FEW ? 2 * kMpPlaceThreads : kMpPlaceThreads, FEW ? 2 : 4) mp_place_kernel(const MpPlaceParams p) {
   constexpr int kThreads = FEW ? 2 * kMpPlaceThreads : kMpPlaceThreads, kRows = FEW ? 2 : 4;

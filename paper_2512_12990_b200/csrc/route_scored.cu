@@ -9,7 +9,7 @@
 // of the selection is then a warp maximum of the lanes' first keys, a ballot for the lowest lane that has it, and a shift in that
 // lane.  Which expert a selected key belongs to is looked up at the end, for all selections side by side.  A group that is made of
 // whole lanes has its two largest keys from the sorted ones by exchanges, and is kept or dropped by lanes.  (Rounds that look through
-// all of a lane's keys, and groups scanned in shared memory, took 1,930 instructions a token and 30 us; now 15.6 in a graph, half of the
+// all of a lane's keys, and groups scanned in shared memory, took 1,930 instructions a token and 30 us; now 1,070 and 15.9 us in a graph, half of the
 // issue slots.)
 #include "mx4.cuh"
 #include "route.cuh"
@@ -17,7 +17,7 @@
 namespace slicemoe {
 
 // Error of an fp32 key.  Sigmoid s = 1 / (1 + t), t = __expf(-l), off by (2 + 1.2 |l|) 2^-23 relative, which enters s with s (1 - s):
-// below 0.6 x 2^-23 for every l; 1 + t rounds by 2^-24 s, __fdividef by 2 ulp, 2^-22 s; adding the bias by 2^-24 |key|: below
+// below 0.64 x 2^-23 for every l; 1 + t rounds by 2^-24 s, __fdividef by 2 ulp, 2^-22 s; adding the bias by 2^-24 |key|: below
 // 2^-21.1 max(1, |key|), two keys 2^-20.1.  Softmax p = e^-d / sum: d rounds by 2^-24 d and d e^-d < 0.37; expf's 2 ulp and the sum's (16 terms
 // in a row, then 5 exchanges: at most 21 roundings of 2^-24, and expf's), the reciprocal and the product 2^-24 each: below 2^-18.9 p +
 // 0.37 x 2^-24, two keys 2^-17.8.
